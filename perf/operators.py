@@ -357,7 +357,8 @@ def _run_own(st):
         return {"k": k, "v": v}
     if c["op"] == "attend":
         if "workspace" not in st:
-            st["workspace"] = cache.attend_workspace(c["batch"], c["nodes"], c["hq"], c["hi"] + c["nodes"])
+            st["workspace"] = cache.attend_workspace(c["batch"], c["nodes"], c["hq"], c["hi"] + c["nodes"],
+                                                     dtype=st["q"].dtype)
         return {"out": cache.attend(st["pages"], st["lens"], st["q"], mask=st["mask"], counts=st["counts"],
                                     max_len=c["hi"] + c["nodes"], out=st["out"], workspace=st["workspace"])}
     from paper_2509_20416_amd import commit_accepted
