@@ -49,7 +49,8 @@ typedef enum {
   FE_E_HIP = 5          /* a HIP runtime call failed */
 } fe_status;
 
-typedef enum { FE_F32 = 0, FE_BF16 = 1 } fe_dtype;
+/* FE_F8 is a storage type of paged caches alone (fe_paged_kv). */
+typedef enum { FE_F32 = 0, FE_BF16 = 1, FE_F8 = 2 } fe_dtype;
 
 /* What cascade layer i attends to, besides its prefix KV cache (the paper's
  * architecture figure is not available; Eq. 2 and Section 2.1 are read as):
@@ -484,6 +485,190 @@ fe_status fe_test_philox_uniforms(const uint64_t *seed_offset, uint64_t first, i
 fe_status fe_test_attn_split(const int32_t *prefix_lens, int32_t batch, int32_t ncols,
                              int32_t nch_ld, int32_t pmax, int32_t waves, int32_t *pieces,
                              int32_t max_pieces, int32_t *n_pieces);
+
+/* ---- the target side of a verification step ------------------------------------
+ *
+ * Tree-attention verification (Section 2.4) runs the target model once over the
+ * nodes of every sequence's draft tree.  The calls below carry its attention
+ * layers: fe_cache_append rotates the nodes' queries and keys and writes keys
+ * and values into the layer's paged cache, fe_tree_attention lets every node see
+ * its sequence's prefix and its own ancestors (fe_tree_out.mask), and after
+ * acceptance fe_cache_commit moves the accepted path's rows behind the prefix in
+ * every layer at once.  fe_cache_gather reads rows back as the packed arrays of
+ * an fe_kv_view.  Plain decoding (one node per sequence) and prompt chunks (a
+ * causal run of nodes) are the same calls.
+ *
+ * They take no handle: the target's shapes are the caller's.  They launch on the
+ * current device, which must be the stream's; they hold no state, so calls are
+ * independent unless they share buffers (a workspace, a cache that one of them
+ * writes).  None allocates or synchronises, and every one may be captured into a
+ * HIP graph. */
+
+/* One layer's paged cache.  A page is page_rows consecutive rows of the pool;
+ * position p of sequence b sits in row
+ *   pages[b][p / page_rows] * page_rows + p % page_rows.
+ * FE_F8: a row holds, per KV head, D codes of OCP e4m3 (1 sign, 4 exponent, 3
+ * mantissa bits, largest 448, no infinities) and one scale byte s for its keys
+ * and one for its values: the values are code * 2^(s - 127).  A power of two
+ * keeps reading back exact (code * 2^(s - 127) is a bf16 value). */
+typedef struct {
+  void *k, *v;        /* [n_pages * page_rows, H_kv, D] in dtype, 16-byte aligned */
+  uint8_t *k_scale, *v_scale; /* FE_F8 only, else ignored: [H_kv, n_pages * page_rows], 4-byte aligned */
+  int32_t n_pages;
+  int32_t page_rows;  /* a power of two, 16 .. 65536 */
+  int32_t n_kv_heads; /* 1 .. 256 */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t dtype;      /* FE_F32, FE_BF16 or FE_F8 */
+} fe_paged_kv;
+
+/* Which pages a batch's sequences own. */
+typedef struct {
+  const int32_t *pages; /* device [B, max_pages] page ids, in position order */
+  int32_t max_pages;
+  int32_t max_len;      /* HOST bound on every position a call touches, plus one:
+                           1 .. max_pages * page_rows */
+} fe_page_table;
+
+/* Rotary positions.  Pair m of a head turns by position * freqs[m] (formed and
+ * reduced in double precision, so far positions lose nothing) and is scaled by
+ * magnitude: (a, b) -> magnitude * (a cos - b sin, b cos + a sin).  FE_ROPE_HALF
+ * pairs dims (m, m + rotary_dim / 2), FE_ROPE_INTERLEAVED dims (2m, 2m + 1), for
+ * m < rotary_dim / 2; dims from rotary_dim on stay as they are. */
+typedef enum { FE_ROPE_HALF = 0, FE_ROPE_INTERLEAVED = 1 } fe_rope_layout;
+typedef struct {
+  const double *freqs; /* device [rotary_dim / 2], radians per position, 8-byte aligned */
+  int32_t rotary_dim;  /* a multiple of 16, 16 .. head_dim */
+  int32_t layout;      /* fe_rope_layout */
+  float magnitude;     /* factor on cosine and sine, positive and finite (1: plain rotation) */
+} fe_rope;
+
+/* Frequencies for fe_rope, HOST arithmetic only: w_m = theta^(-2m / rotary_dim),
+ * m < rotary_dim / 2, scaled for contexts longer than the trained one:
+ *  FE_SCALE_NONE
+ *  FE_SCALE_LINEAR  w_m / factor (position interpolation)
+ *  FE_SCALE_BANDED  by the turns t = trained_len * w_m / 2 pi that a pair makes
+ *    over the trained context: with s = clamp((t - low) / (high - low), 0, 1),
+ *    (1 - s) * w_m / factor + s * w_m
+ *  FE_SCALE_RAMP    by the pair's index: with i(t) = rotary_dim *
+ *    ln(trained_len / (2 pi t)) / (2 ln theta), a = max(floor(i(high)), 0), b =
+ *    min(ceil(i(low)), rotary_dim / 2 - 1) (a + 0.001 if not above a) and r =
+ *    clamp((m - a) / (b - a), 0, 1), w_m / factor * r + w_m * (1 - r); the
+ *    magnitude is 0.1 ln(factor) + 1 (published as YaRN)
+ * freqs: HOST [rotary_dim / 2]; magnitude: HOST, 1 except for FE_SCALE_RAMP.
+ * factor, low, high and trained_len are read where the formula has them.
+ * Errors: FE_E_INVALID (NULL outputs, rotary_dim not a positive even number,
+ * theta not above 1 or not finite, an unknown scaling, factor below 1, low not
+ * positive or not below high, trained_len < 1). */
+typedef enum { FE_SCALE_NONE = 0, FE_SCALE_LINEAR = 1, FE_SCALE_BANDED = 2, FE_SCALE_RAMP = 3 } fe_rope_scaling;
+fe_status fe_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor,
+                              double low, double high, double trained_len, double *freqs,
+                              float *magnitude);
+
+/* Appends the rows of `nodes` new positions per sequence to a cache, queries and
+ * keys rotated on the way.  Row (b, i), i < counts[b], goes to position
+ * starts[b] + i of sequence b (its place in the cache) and turns at
+ * positions[b][i] (a tree node's is the prefix length plus its depth).
+ *  k, v   [B, nodes, H_kv, D] in dtype, row (b, i) at element (b * nodes + i) *
+ *         stride (so that parts of a joint projection can be passed as they are);
+ *         16-byte aligned, strides multiples of 16 bytes and at least H_kv * D
+ *  q      optional, [B, nodes, n_q_heads, D] likewise (n_q_heads: 1 .. 1024);
+ *         q_out [B, nodes, n_q_heads, D] dense, not overlapping q
+ *  starts [B] int32; counts [B] int32 or NULL (all nodes); positions [B, nodes]
+ *         int32 or NULL (starts[b] + i)
+ *  rope   NULL: no rotation
+ *  dtype  FE_BF16 or FE_F32; the cache's dtype is the same or FE_F8
+ * Rotated values are formed in fp32 for bf16 results and in double for fp32 and
+ * FE_F8 ones (rounded to fp32, then coded: s is the smallest of 1 .. 254 with
+ * max|y| <= 448 * 2^(s - 127) over the row's head, code = e4m3(y * 2^(127 - s)),
+ * ties to even; values that are not finite are left out of the maximum and
+ * stored as NaN).
+ * Device-side values the host cannot check: rows from counts[b] on are not
+ * touched (in q_out neither); a row whose position in the cache lies outside [0,
+ * max_len) or on a page outside [0, n_pages) is not written to the cache (its
+ * q_out row is).  Rows that share a cache row race.  Errors: FE_E_INVALID (NULL
+ * or bad arguments), FE_E_UNSUPPORTED (head_dim, page_rows, dtype pairs,
+ * rotary_dim), FE_E_ALIGN; nothing is launched on an error.  batch == 0 or
+ * nodes == 0 is a no-op. */
+fe_status fe_cache_append(const fe_paged_kv *cache, const fe_page_table *table, int32_t batch,
+                          int32_t nodes, const int32_t *starts, const int32_t *counts,
+                          const int32_t *positions, const fe_rope *rope, int32_t dtype,
+                          const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                          const void *q, int64_t q_stride, int32_t n_q_heads, void *q_out,
+                          void *stream);
+
+/* Reads cache rows back as packed arrays: row r of the outputs, cu_rows[b] <= r <
+ * cu_rows[b + 1], is position starts[b] + r - cu_rows[b] of sequence b (starts
+ * NULL: from position 0, so that the result is an fe_kv_view's cache with
+ * cu_prefix = cu_rows).
+ *  k_out, v_out [n_rows, H_kv, D] in dtype (FE_BF16 or FE_F32), 16-byte aligned;
+ *               either may be NULL
+ *  cu_rows      [B + 1] int32, not decreasing
+ * Values are rounded once, to nearest even, where dtype is narrower.  A position
+ * outside [0, max_len) or on a page outside [0, n_pages) gives a NaN row; output
+ * rows outside [cu_rows[0], cu_rows[B]) are left as they were.  Errors:
+ * FE_E_INVALID, FE_E_UNSUPPORTED, FE_E_ALIGN; nothing is launched on an error.
+ * n_rows == 0 is a no-op. */
+fe_status fe_cache_gather(const fe_paged_kv *cache, const fe_page_table *table, int32_t batch,
+                          const int32_t *starts, const int32_t *cu_rows, int32_t n_rows,
+                          int32_t dtype, void *k_out, void *v_out, void *stream);
+
+/* Attention of tree nodes over a paged cache (Section 2.4).  Sequence b has
+ * P = prefix_lens[b] verified positions and n = counts[b] nodes (NULL: all
+ * `nodes`) whose keys and values sit at positions P .. P + n - 1, node order
+ * (fe_cache_append wrote them).  Node a sees the prefix and the nodes c < n with
+ * mask[b][a][c] != 0 (mask NULL: c <= a, a causal run):
+ *   out[b][a][h] = sum_j softmax_j(scale * q[b][a][h] . k_j) v_j,
+ * head h reading KV head h / (n_q_heads / H_kv).  A node that sees nothing gets
+ * zeros; what a node does not see never matters, infinities and NaN included.
+ * The sums are fp32; in bf16 the probabilities are rounded to bf16 as they enter
+ * the product with the values and in the sum that divides it.
+ *  q    [B, nodes, n_q_heads, D] in dtype (FE_BF16 or FE_F32; the cache's dtype is
+ *       the same or FE_F8), rotated, row (b, a) at element (b * nodes + a) *
+ *       q_stride; 16-byte aligned, q_stride a multiple of 16 bytes
+ *  out  [B, nodes, n_q_heads, D] dense in dtype, 16-byte aligned, not overlapping q
+ *  mask [B, nodes, nodes] uint8 or NULL
+ *  scale  positive and finite (usually 1 / sqrt(D))
+ *  workspace  device memory, 256-byte aligned, at least
+ *       fe_tree_attention_workspace_bytes; calls in flight together need one each
+ * Device-side values the host cannot check: a sequence with P < 0, n outside [0,
+ * nodes] or P + n > max_len reads no cache row and its live rows (all, where n is
+ * bad) become NaN; a key on a page outside [0, n_pages) is NaN to the nodes that
+ * see it.  Rows from counts[b] on are left as they were.  n_q_heads is a multiple
+ * of H_kv, at most 1024; nodes * n_q_heads / H_kv at most 2^20.  Errors:
+ * FE_E_INVALID, FE_E_UNSUPPORTED, FE_E_ALIGN, FE_E_WORKSPACE; nothing is launched
+ * on an error.  batch == 0 or nodes == 0 is a no-op. */
+fe_status fe_tree_attention(const fe_paged_kv *cache, const fe_page_table *table, int32_t batch,
+                            int32_t nodes, int32_t n_q_heads, const int32_t *prefix_lens,
+                            const int32_t *counts, const uint8_t *mask, int32_t dtype,
+                            const void *q, int64_t q_stride, float scale, void *out,
+                            void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace (bytes) of the same call (0 if it would be refused). */
+size_t fe_tree_attention_workspace_bytes(const fe_paged_kv *cache, const fe_page_table *table,
+                                         int32_t batch, int32_t nodes, int32_t n_q_heads,
+                                         int32_t dtype);
+
+/* Moves the accepted nodes' rows behind the prefix in the caches of n_layers
+ * layers: with P = prefix_lens[b], path = retrieve[b][accept_path[b]] and len =
+ * accept_len[b] (as fe_accept_greedy / fe_accept_sample leave them), position
+ * P + t takes what position P + path[t] held before the call, t = 1 .. len (keys
+ * are rotated by depth, so they stay right), and new_lens[b] = P + 1 + len: the
+ * root and the accepted nodes are verified.
+ *  caches   HOST array [n_layers] (1 .. 1024), all of one shape, one page table
+ *  retrieve [B, n_paths, depth + 1] int32 (fe_tree_out.retrieve), depth 0 .. 16
+ *  prefix_lens, accept_path, accept_len [B] int32; new_lens [B] int32, not
+ *           overlapping them
+ * A sequence with accept_len outside [0, depth], accept_path outside [0,
+ * n_paths), a path node 1 .. len outside [0, nodes), or one of the positions
+ * involved outside [0, max_len) or on a page outside [0, n_pages) keeps its rows,
+ * and its new_lens becomes -1 (so that later calls give NaN, not wrong rows).
+ * Errors: FE_E_INVALID, FE_E_UNSUPPORTED, FE_E_ALIGN; nothing is launched on an
+ * error.  batch == 0 is a no-op. */
+fe_status fe_cache_commit(const fe_paged_kv *caches, int32_t n_layers, const fe_page_table *table,
+                          int32_t batch, int32_t nodes, int32_t n_paths, int32_t depth,
+                          const int32_t *prefix_lens, const int32_t *retrieve,
+                          const int32_t *accept_path, const int32_t *accept_len,
+                          int32_t *new_lens, void *stream);
 
 void fe_drafter_destroy(fe_drafter *h);
 

@@ -11,16 +11,17 @@
 #include <new>
 #include <vector>
 
-#include <rocprofiler-sdk-roctx/roctx.h>
-
-#include "../../include/fe.h"
-#include "fe_internal.h"
+#include "fe_host.h"
 
 using namespace fe;
 
 namespace {
 
 thread_local char g_err[512];
+
+}  // namespace
+
+namespace fe {
 
 fe_status fail(fe_status st, const char *fmt, ...) {
   va_list ap;
@@ -30,25 +31,11 @@ fe_status fail(fe_status st, const char *fmt, ...) {
   return st;
 }
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+}  // namespace fe
 
-#define FE_TRY(x)                                                           \
-  do {                                                                      \
-    hipError_t e_ = (x);                                                    \
-    if (e_ != hipSuccess) return fail(FE_E_HIP, "%s: %s", #x, hipGetErrorString(e_)); \
-  } while (0)
+namespace {
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// A roctx range over a host scope: the entry points, the pass and its layers
-// show up by name on a rocprofv3 --marker-trace timeline (host time: when the
-// work was enqueued, or captured).
-struct Range {
-  explicit Range(const char *name) { roctxRangePushA(name); }
-  ~Range() { roctxRangePop(); }
-  Range(const Range &) = delete;
-  Range &operator=(const Range &) = delete;
-};
 
 struct Layout {
   size_t cat, X, Xp, ssqX, ssqP, AQ, AM, AF, an, bn, q, knew, vnew, part, rope, ao, s, pmax,

@@ -15,8 +15,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("FE_LIBRARY") or os.path.join(HERE, "libfe.so")
 
 FE_OK, FE_E_INVALID, FE_E_UNSUPPORTED, FE_E_ALIGN, FE_E_WORKSPACE, FE_E_HIP = range(6)
-FE_F32, FE_BF16 = 0, 1
+FE_F32, FE_BF16, FE_F8 = 0, 1, 2
 FE_CTX_CASCADE, FE_CTX_SELF, FE_CTX_PARALLEL = 0, 1, 2
+FE_ROPE_HALF, FE_ROPE_INTERLEAVED = 0, 1
+FE_SCALE_NONE, FE_SCALE_LINEAR, FE_SCALE_BANDED, FE_SCALE_RAMP = range(4)
 STATUS_NAMES = {0: "FE_OK", 1: "FE_E_INVALID", 2: "FE_E_UNSUPPORTED", 3: "FE_E_ALIGN",
                 4: "FE_E_WORKSPACE", 5: "FE_E_HIP"}
 
@@ -25,7 +27,9 @@ EXPORTS = ("fe_workspace_bytes", "fe_drafter_create", "fe_draft_forward", "fe_dr
            "fe_draft_sample_seeded", "fe_build_tree",
            "fe_accept_greedy", "fe_accept_sample", "fe_accept_sample_seeded", "fe_kv_update_workspace_bytes", "fe_kv_update", "fe_kv_update_noalloc", "fe_set_graph_mode", "fe_set_attention_split", "fe_time_stage", "fe_set_pass_mode", "fe_pass_status",
            "fe_drafter_destroy", "fe_last_error", "fe_test_attn_split", "fe_test_philox_uniforms",
-           "fe_test_attention", "fe_test_rmsnorm")
+           "fe_test_attention", "fe_test_rmsnorm", "fe_rope_frequencies", "fe_cache_append",
+           "fe_cache_gather", "fe_tree_attention", "fe_tree_attention_workspace_bytes",
+           "fe_cache_commit")
 FE_STAGE = dict(fuse=0, input=1, qkv=2, attn=3, oproj=4, gateup=5, down=6, lmhead=7, pass_=8)
 
 
@@ -67,6 +71,21 @@ class fe_draft_out(C.Structure):
     _fields_ = [("topk_ids", C.c_void_p), ("topk_probs", C.c_void_p), ("topk_draft", C.c_void_p),
                 ("logits", C.c_void_p), ("hidden", C.c_void_p),
                 ("tree", C.POINTER(fe_tree_out))]
+
+
+class fe_paged_kv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_rows", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class fe_page_table(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("max_pages", C.c_int32), ("max_len", C.c_int32)]
+
+
+class fe_rope(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("rotary_dim", C.c_int32), ("layout", C.c_int32),
+                ("magnitude", C.c_float)]
 
 
 _lib = None
@@ -142,6 +161,22 @@ def lib() -> C.CDLL:
         L.fe_test_attn_split.restype = C.c_int
         L.fe_test_attn_split.argtypes = [C.c_void_p] + [C.c_int32] * 5 + [C.c_void_p, C.c_int32,
                                                                          C.c_void_p]
+        i32, i64, vp = C.c_int32, C.c_int64, C.c_void_p
+        kv, tab = C.POINTER(fe_paged_kv), C.POINTER(fe_page_table)
+        L.fe_rope_frequencies.restype = C.c_int
+        L.fe_rope_frequencies.argtypes = [i32, C.c_double, i32] + [C.c_double] * 4 + [vp, vp]
+        L.fe_cache_append.restype = C.c_int
+        L.fe_cache_append.argtypes = [kv, tab, i32, i32, vp, vp, vp, C.POINTER(fe_rope), i32, vp, i64,
+                                      vp, i64, vp, i64, i32, vp, vp]
+        L.fe_cache_gather.restype = C.c_int
+        L.fe_cache_gather.argtypes = [kv, tab, i32, vp, vp, i32, i32, vp, vp, vp]
+        L.fe_tree_attention.restype = C.c_int
+        L.fe_tree_attention.argtypes = [kv, tab, i32, i32, i32, vp, vp, vp, i32, vp, i64, C.c_float, vp,
+                                        vp, C.c_size_t, vp]
+        L.fe_tree_attention_workspace_bytes.restype = C.c_size_t
+        L.fe_tree_attention_workspace_bytes.argtypes = [kv, tab, i32, i32, i32, i32]
+        L.fe_cache_commit.restype = C.c_int
+        L.fe_cache_commit.argtypes = [kv, i32, tab, i32, i32, i32, i32] + [vp] * 6
         L.fe_drafter_destroy.restype = None
         L.fe_drafter_destroy.argtypes = [C.c_void_p]
         L.fe_last_error.restype = C.c_char_p
@@ -323,3 +358,46 @@ def fe_test_rmsnorm(dtype: int, x: int, rows: int, d: int, gamma: int, eps: floa
                     stream: int) -> None:
     check(lib().fe_test_rmsnorm(dtype, C.c_void_p(x), rows, d, C.c_void_p(gamma), C.c_float(eps),
                                 C.c_void_p(out), C.c_void_p(stream)))
+
+
+def fe_rope_frequencies(rotary_dim: int, theta: float, scaling: int = FE_SCALE_NONE, factor: float = 1.0,
+                        low: float = 0.0, high: float = 0.0, trained_len: float = 0.0):
+    """(radians per position as float64 [rotary_dim / 2], magnitude), on the host."""
+    import numpy as np
+    out = np.zeros(max(1, int(rotary_dim) // 2), np.float64)
+    mag = C.c_float()
+    check(lib().fe_rope_frequencies(int(rotary_dim), float(theta), int(scaling), float(factor), float(low),
+                                    float(high), float(trained_len), out.ctypes.data, C.addressof(mag)))
+    return out, float(mag.value)
+
+
+def fe_cache_append(cache: fe_paged_kv, table: fe_page_table, batch: int, nodes: int, starts, counts, positions,
+                    rope, dtype: int, k, k_stride: int, v, v_stride: int, q, q_stride: int, n_q_heads: int,
+                    q_out, stream: int) -> None:
+    """rope: an fe_rope or None; pointers as ints, None for NULL."""
+    check(lib().fe_cache_append(cache, table, batch, nodes, starts, counts, positions, rope, dtype, k, k_stride,
+                                v, v_stride, q, q_stride, n_q_heads, q_out, stream))
+
+
+def fe_cache_gather(cache: fe_paged_kv, table: fe_page_table, batch: int, starts, cu_rows, n_rows: int,
+                    dtype: int, k_out, v_out, stream: int) -> None:
+    check(lib().fe_cache_gather(cache, table, batch, starts, cu_rows, n_rows, dtype, k_out, v_out, stream))
+
+
+def fe_tree_attention(cache: fe_paged_kv, table: fe_page_table, batch: int, nodes: int, n_q_heads: int,
+                      prefix_lens, counts, mask, dtype: int, q, q_stride: int, scale: float, out, workspace,
+                      ws_bytes: int, stream: int) -> None:
+    check(lib().fe_tree_attention(cache, table, batch, nodes, n_q_heads, prefix_lens, counts, mask, dtype, q,
+                                  q_stride, scale, out, workspace, ws_bytes, stream))
+
+
+def fe_tree_attention_workspace_bytes(cache: fe_paged_kv, table: fe_page_table, batch: int, nodes: int,
+                                      n_q_heads: int, dtype: int) -> int:
+    return int(lib().fe_tree_attention_workspace_bytes(cache, table, batch, nodes, n_q_heads, dtype))
+
+
+def fe_cache_commit(caches, n_layers: int, table: fe_page_table, batch: int, nodes: int, n_paths: int, depth: int,
+                    prefix_lens, retrieve, accept_path, accept_len, new_lens, stream: int) -> None:
+    """caches: a ctypes array of fe_paged_kv, one per layer."""
+    check(lib().fe_cache_commit(caches, n_layers, table, batch, nodes, n_paths, depth, prefix_lens, retrieve,
+                                accept_path, accept_len, new_lens, stream))
