@@ -526,7 +526,7 @@ typedef struct {
   const int32_t *pages; /* device [B, max_pages] page ids, in position order */
   int32_t max_pages;
   int32_t max_len;      /* HOST bound on every position a call touches, plus one:
-                           1 .. max_pages * page_rows */
+                           1 .. max_pages * page_rows, at most 2^30 */
 } fe_page_table;
 
 /* Rotary positions.  Pair m of a head turns by position * freqs[m] (formed and

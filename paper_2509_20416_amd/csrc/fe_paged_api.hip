@@ -40,6 +40,7 @@ fe_status check_table(const fe_paged_kv *c, const fe_page_table *t) {
   if (!aligned4(t->pages)) return fail(FE_E_ALIGN, "page ids must be 4-byte aligned");
   if (t->max_pages < 1 || t->max_len < 1 || t->max_len > (int64_t)t->max_pages * c->page_rows)
     return fail(FE_E_INVALID, "max_len %d outside [1, max_pages * page_rows]", t->max_len);
+  if (t->max_len > 1 << 30) return fail(FE_E_UNSUPPORTED, "max_len > 2^30");
   return FE_OK;
 }
 

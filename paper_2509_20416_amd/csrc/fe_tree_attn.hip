@@ -1,90 +1,688 @@
 // fe_tree_attn.hip -- attention of draft-tree nodes over a paged cache (gfx950).
+//
+// The T * G rows of one (sequence, KV head) -- its nodes times the G query heads
+// that share the KV head -- read the same keys, so they are the columns of one
+// pair of matrix products over the cache: S^T = K Q^T, O^T = V^T P^T.  A
+// workgroup takes a tile of TR = 32 RW of these rows and walks the keys once,
+// with the running maximum and sum of a softmax per row.
+//
+//  * In the 32x32 accumulators a lane holds 16 keys of one row, which is what the
+//    second product wants as its right operand once V's keys are taken in the
+//    same order: probabilities never move between lanes, and a row's maximum and
+//    sum need one exchange, with lane ^ 32.
+//  * Keys go through registers into LDS: a tile is loaded (16 bytes a lane, its
+//    pages looked up one tile ahead) while the one before is worked on, and 8-bit
+//    codes become bf16 (or fp32) there, once per workgroup.  With a power of two
+//    as the scale that is exact.
+//  * RW waves share a tile, side by side on rows; KW groups of them take the
+//    tiles in turn and add up at the end.  Few rows: RW = 1, every wave streams
+//    its own keys, which is a matter of bytes.  Many: RW = 4, each key is read
+//    once per 128 rows.
+//  * The tiles of all (sequence, row tile, KV head) segments are numbered and cut
+//    into equal ranges, one per workgroup, whatever the lengths: a segment that
+//    ranges share leaves partial sums, joined in order by a second launch.  A
+//    range leaves at most two partials (the segment it starts in and the one it
+//    ends in), so their number does not depend on the lengths either.
+//  * Only tiles that reach past what every row of the tile sees are masked.  A
+//    masked score is replaced, so what it was does not matter; in a value row an
+//    infinity or NaN would still come through as 0 * inf, so a masked tile that
+//    holds one is added key by key, each row over the keys it sees.
+#include <algorithm>
+#include <atomic>
+
+#include "fe_attn_unit.h"
 #include "fe_paged.h"
 
 namespace fe {
 namespace {
 
-// One wave per (sequence, node, query head): a key at a time, its score summed
-// over the wave, running maximum and sum.
-template <typename T, typename S, int D>
-__global__ __launch_bounds__(256) void k_tree_attn_rows(TreeArgs a) {
-  constexpr int E = D / 64;
-  const PagedView &c = a.c;
-  const long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Shape of one variant: RW waves side by side on rows, KW groups of them taking
+// tiles of TK keys in turn.
+template <typename T, int D, int RW_, int KW_> struct Shape {
+  static constexpr int RW = RW_, KW = KW_;
+  static constexpr int TK = RW >= 4 ? 64 : 32;   // keys per tile
+  static constexpr int IK = TK * KW;             // keys per work item
+  static constexpr int TR = 32 * RW;             // rows per tile
+  static constexpr int NT = 64 * RW * KW;        // threads
+  static constexpr int NBUF = RW == 1 ? 1 : 2;   // LDS buffers per group
+  static constexpr int RB = D * (int)sizeof(T);  // bytes per row in LDS
+  static constexpr int BUF = 2 * TK * RB;        // K rows, then V rows
+  static constexpr int LDS = KW * NBUF * BUF;
+};
+
+// ---- the split ------------------------------------------------------------------
+
+// One sequence's rows and keys as a row tile sees them.
+struct Span {
+  int P, n, live;  // prefix, nodes, rows that get written
+  bool bad;
+};
+__device__ __forceinline__ Span span_of(const TreeArgs &a, int b) {
+  Span s;
+  s.P = a.lens[b];
+  s.n = a.counts ? a.counts[b] : a.T;
+  const bool nbad = s.n < 0 || s.n > a.T;
+  if (nbad) s.n = a.T;
+  s.bad = nbad || s.P < 0 || (long)s.P + s.n > a.c.max_len;
+  s.live = s.n * (a.Hq / a.c.Hkv);
+  return s;
+}
+// Keys that row tile rt (TR rows) of a sequence reads: [0, end); every row of it
+// sees [0, all).
+__device__ __forceinline__ int keys_end(const TreeArgs &a, const Span &s, int rt, int TR) {
+  if (s.bad) return 0;
+  if (a.mask) return s.P + s.n;
+  return s.P + (min((rt + 1) * TR, s.live) - 1) / (a.Hq / a.c.Hkv) + 1;
+}
+// Work items of a segment (none where the tile has no row).
+__device__ __forceinline__ int items_of(const TreeArgs &a, int e, int nrt, int TR, int IK) {
+  const Span s = span_of(a, e / nrt);
+  const int rt = e % nrt;
+  if (rt * TR >= s.live) return 0;
+  return max(1, (keys_end(a, s, rt, TR) + IK - 1) / IK);
+}
+
+__device__ __forceinline__ long wave_incl_scan(long x) {
   const int lane = threadIdx.x & 63;
-  if (w >= (long)a.B * a.T * a.Hq) return;
-  const int h = w % a.Hq, t = w / a.Hq % a.T, b = w / a.Hq / a.T, hk = h / (a.Hq / c.Hkv);
-  const int P = a.lens[b], n = a.counts ? a.counts[b] : a.T;
-  const bool bad = P < 0 || n < 0 || n > a.T || (long)P + n > c.max_len;
-  if (n >= 0 && n <= a.T && t >= n) return;
-  T *out = (T *)a.out + (((long)b * a.T + t) * a.Hq + h) * D + E * lane;
-  const T *qp = (const T *)a.q + ((long)b * a.T + t) * a.qs + (long)h * D + E * lane;
-  float q[E], o[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = Elt<T>::to_f(qp[e]) * (a.scale * 1.4426950408889634f);
-    o[e] = 0.f;
+  for (int o = 1; o < 64; o <<= 1) {
+    const long y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
   }
-  float m = -INFINITY, l = 0.f;
-  const int end = bad ? 0 : P + n;
-  for (int j = 0; j < end; ++j) {
-    const int node = j - P;
-    if (node >= 0 && !(a.mask ? a.mask[((long)b * a.T + t) * a.T + node] != 0 : node <= t)) continue;
-    const long row = c.row(b, j);
-    float k[E], v[E];
-    if (row < 0) {
+  return x;
+}
+
+// Equal ranges of `total` items over W workgroups; none is empty (W is at most
+// total), so every range between a segment's first and last holds a part of it.
+struct Ranges {
+  long total, W;
+  __device__ __forceinline__ Ranges(long items, int wgs) : total(items), W(items < wgs ? items : wgs) {}
+  __device__ __forceinline__ long begin(long w) const { return total * w / W; }
+  // the range that holds item x
+  __device__ __forceinline__ long owner(long x) const {
+    const long w = ((x + 1) * W + total - 1) / total - 1;
+    return w < W - 1 ? w : W - 1;
+  }
+};
+
+// Workspace: per range two partials (slot 2w: the segment the range starts inside
+// of, 2w + 1: the one it ends inside of), o [TR][D] and (max, sum) [TR] each; then
+// the items before every (sequence, row tile), E + 1 of them.
+template <int D> struct Work {
+  float *p;
+  long slots;
+  int TR;
+  __host__ __device__ float *o(long slot) const { return p + slot * TR * D; }
+  __host__ __device__ float *ml(long slot) const { return p + slots * TR * D + slot * TR * 2; }
+  __host__ __device__ long *before() const { return (long *)(p + slots * TR * (D + 2)); }
+};
+
+// ---- one tile of keys: global memory -> registers -> LDS ---------------------------
+
+// 16-byte piece p of row R (rows of VPR pieces) in LDS: pieces are permuted within
+// a row so that sixteen rows' reads of one piece meet sixteen different banks, and
+// so do four rows' reads of four neighbouring pieces (the transposing read).
+template <int VPR> __device__ __forceinline__ int piece_at(int R, int p) {
+  if constexpr (VPR == 8)
+    return R * 8 + (p ^ ((((R >> 1) & 1) << 2) | ((R >> 2) & 3)));
+  else
+    return R * VPR + (p ^ (((R & 3) << 2) | ((R >> 2) & 3)));
+}
+
+template <typename T, typename S, int D, int RW, int TK> struct Tile {
+  static constexpr int PS = D * (int)sizeof(S) / 16;  // 16-byte pieces of a stored row
+  static constexpr int VPR = D * (int)sizeof(T) / 16;
+  static constexpr int STEP = 64 * RW / PS;           // rows between a thread's loads
+  static constexpr int NL = TK / STEP;                // loads per thread, K (as many V)
+  static_assert(STEP >= 1 && NL >= 1 && TK % STEP == 0, "whole loads");
+  static constexpr int NP = STEP >= 16 ? NL : TK / 16;  // pages per thread: rows of one page share it
+  static constexpr bool F8 = sizeof(S) == 1;
+  u32x4 k[NL], v[NL];
+  uint32_t sk[NL], sv[NL];  // scale bytes
+  int pid[NP];
+  uint32_t badp;  // bit i: load i's page lies outside the pool
+
+  __device__ __forceinline__ int row(int i, int tg) const { return i * STEP + tg / PS; }
+
+  __device__ __forceinline__ void pages(const PagedView &c, const int32_t *table, int k0, int end, int tg) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) k[e] = v[e] = __int_as_float(0x7fc00000);
+    for (int j = 0; j < NP; ++j) {
+      const int R = STEP >= 16 ? row(j, tg) : 16 * j + tg / PS;
+      pid[j] = table[min(k0 + R, end - 1) >> c.shift];
+    }
+  }
+  // `pages` has run for the same k0.  Rows past end are loaded clamped.
+  __device__ __forceinline__ void load(const PagedView &c, int hk, int k0, int end, int tg) {
+    badp = 0;
+    const long rowb = (long)c.Hkv * D * sizeof(S);
+    const int off = hk * D * (int)sizeof(S) + 16 * (tg % PS);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int pos = min(k0 + row(i, tg), end - 1);
+      const int pg = pid[STEP >= 16 ? i : i * STEP / 16];
+      const bool ok = (unsigned)pg < (unsigned)c.n_pages;
+      if (!ok) badp |= 1u << i;
+      const long r = ((long)(ok ? pg : 0) << c.shift) + (pos & ((1 << c.shift) - 1));
+      k[i] = *reinterpret_cast<const u32x4 *>((const char *)c.k + r * rowb + off);
+      v[i] = *reinterpret_cast<const u32x4 *>((const char *)c.v + r * rowb + off);
+      if constexpr (F8) {
+        sk[i] = c.ks[hk * c.rows() + r];
+        sv[i] = c.vs[hk * c.rows() + r];
+      }
+    }
+  }
+  __device__ __forceinline__ static void put(unsigned char *lds, int R, int p, const u32x4 &w, uint32_t s) {
+    u32x4 *dst = reinterpret_cast<u32x4 *>(lds);
+    if constexpr (!F8) {
+      dst[piece_at<VPR>(R, p)] = w;
     } else {
-      const long at = (row * c.Hkv + hk) * D + E * lane;
-      if constexpr (sizeof(S) == 1) {
-        const float sk = scale_of(c.ks[hk * c.rows() + row]), sv = scale_of(c.vs[hk * c.rows() + row]);
+      const float sc = scale_of(s);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          k[e] = f8x4_to_f(((const uint8_t *)c.k)[at + e]).x * sk;
-          v[e] = f8x4_to_f(((const uint8_t *)c.v)[at + e]).x * sv;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          k[e] = Elt<S>::to_f(((const S *)c.k)[at + e]);
-          v[e] = Elt<S>::to_f(((const S *)c.v)[at + e]);
+      for (int q = 0; q < 2; ++q) {
+        const f32x4 a = f8x4_to_f(w[2 * q]) * sc, b = f8x4_to_f(w[2 * q + 1]) * sc;
+        if constexpr (sizeof(T) == 2) {
+          dst[piece_at<VPR>(R, 2 * p + q)] = u32x4{f2bf2(a.x, a.y), f2bf2(a.z, a.w), f2bf2(b.x, b.y), f2bf2(b.z, b.w)};
+        } else {
+          dst[piece_at<VPR>(R, 4 * p + 2 * q)] = __builtin_bit_cast(u32x4, a);
+          dst[piece_at<VPR>(R, 4 * p + 2 * q + 1)] = __builtin_bit_cast(u32x4, b);
         }
       }
     }
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += q[e] * k[e];
-    s = group_sum<64>(s);
-    const float mn = fmaxf(m, s), al = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    const float p = __builtin_amdgcn_exp2f(s - (mn == -INFINITY ? 0.f : mn));
-    m = mn;
-    l = l * al + p;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * al + p * v[e];
   }
-  const float inv = bad ? __int_as_float(0x7fc00000) : l == 0.f ? 0.f : 1.f / l;
+  // Writes the tile; ragged: rows from `left` on become zeros.  A row on a bad page
+  // becomes NaN keys (and zero values).  Returns whether a value this thread wrote
+  // is not finite (asked for masked tiles only).
+  __device__ __forceinline__ bool store(unsigned char *lds, int tg, int left, bool masked) {
+    bool odd = false;
 #pragma unroll
-  for (int e = 0; e < E; ++e) out[e] = Elt<T>::from_f(o[e] * inv);
+    for (int i = 0; i < NL; ++i) {
+      const int R = row(i, tg);
+      u32x4 kw = k[i], vw = v[i];
+      if (badp >> i & 1) {
+        kw = u32x4(0xffffffffu);
+        vw = u32x4(0u);
+      }
+      if (masked) {
+        if (R >= left) kw = vw = u32x4(0u);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x = vw[w];
+          if constexpr (F8) {
+            const uint32_t y = (x & 0x7f7f7f7fu) + 0x01010101u;  // a NaN code is 127: bit 7 comes up
+            odd |= (y & 0x80808080u) != 0;
+          } else if constexpr (sizeof(S) == 2) {
+            odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+          } else {
+            odd |= (x & 0x7f800000u) == 0x7f800000u;
+          }
+        }
+      }
+      put(lds, R, tg % PS, kw, F8 ? sk[i] : 0);
+      put(lds + TK * D * sizeof(T), R, tg % PS, vw, F8 ? sv[i] : 0);
+    }
+    return odd;
+  }
+};
+
+// ---- the kernel -------------------------------------------------------------------
+
+template <typename T, typename S, int D, int RW, int KW>
+__global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt, int W_) {
+  using Sh = Shape<T, D, RW, KW>;
+  constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / 32;
+  constexpr int VPR = D * (int)sizeof(T) / 16;
+  constexpr int NC = VPR / 2;  // steps of two 16-byte pieces along a key
+  __shared__ __attribute__((aligned(16))) unsigned char s_mem[Sh::LDS];
+  __shared__ float s_ml[KW > 1 ? KW * RW * 64 : 1][2];
+  __shared__ long s_scan[NT / 64 + 1];
+  __shared__ long s_first[2];
+  __shared__ uint32_t s_odd[2][RW * KW];
+  const PagedView &c = a.c;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int grp = wave / RW, rw = wave % RW, tg = rw * 64 + lane;
+  const int n32 = lane & 31, h = lane >> 5;
+  const int G = a.Hq / c.Hkv, E = a.B * nrt;
+  // the items of every segment, this range of them, and the segment it starts in
+  Work<D> work{a.ws, 2L * W_, TR};
+  long total = 0;
+  for (int e0 = 0; e0 < E; e0 += NT) {
+    const long x = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
+    const long inc = wave_incl_scan(x);
+    if (lane == 63) s_scan[wave] = inc;
+    __syncthreads();
+    long base = total;
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < wave) base += s_scan[w];
+      total += s_scan[w];
+    }
+    if (blockIdx.x == 0 && e0 + tid < E) work.before()[e0 + tid] = base + inc - x;
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && tid == 0) work.before()[E] = total;
+  const Ranges rg(total * c.Hkv, W_);
+  if (blockIdx.x >= rg.W) return;
+  // neighbouring ranges on one XCD: workgroups go round the 8 of them
+  const int xcd = blockIdx.x % 8, wg = (int)(xcd * (rg.W / 8) + min((long)xcd, rg.W % 8)) + blockIdx.x / 8;
+  const long x0 = rg.begin(wg), x1 = rg.begin(wg + 1);
+  {
+    long run = 0;
+    for (int e0 = 0; e0 < E; e0 += NT) {
+      const long x = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
+      const long inc = wave_incl_scan(x);
+      if (lane == 63) s_scan[wave] = inc;
+      __syncthreads();
+      long base = run;
+      for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) base += s_scan[w];
+        run += s_scan[w];
+      }
+      const long lo = (base + inc - x) * c.Hkv;
+      if (x > 0 && lo <= x0 && x0 < lo + x * c.Hkv) {
+        s_first[0] = e0 + tid;
+        s_first[1] = lo;
+      }
+      __syncthreads();
+      if (run * c.Hkv > x0) break;
+    }
+  }
+  int e = (int)s_first[0];
+  long at = s_first[1];  // first item of entry e
+  unsigned char *buf = s_mem + grp * Sh::NBUF * Sh::BUF;
+
+  for (long x = x0; x < x1;) {
+    const int it = items_of(a, e, nrt, TR, IK);
+    if (it == 0 || x >= at + (long)it * c.Hkv) {
+      at += (long)it * c.Hkv;
+      ++e;
+      continue;
+    }
+    const int b = e / nrt, rt = e % nrt, hk = (int)((x - at) / it), i0 = (int)((x - at) % it);
+    const int ni = (int)min((long)(it - i0), x1 - x);
+    x += ni;
+    const Span sp = span_of(a, b);
+    const int end = keys_end(a, sp, rt, TR);
+    // this lane's row: node, head
+    const int row = rt * TR + 32 * rw + n32, rowc = min(row, sp.live - 1);
+    const int node = rowc / G, head = hk * G + rowc % G;
+    const int vis_all = sp.P + (a.mask ? 0 : rt * TR / G + 1);  // keys every row sees
+    const int32_t *table = c.pages + (size_t)b * c.max_pages;
+
+    // q, 16 bytes of two neighbouring pieces per step: the right operand
+    u32x4 qf[NC];
+    {
+      const T *qp = (const T *)a.q + ((long)b * a.T + node) * a.qs + (long)head * D;
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) qf[cc] = *reinterpret_cast<const u32x4 *>((const char *)qp + 16 * (2 * cc + h));
+    }
+    f32x16 o[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x16(0.f);
+    float m = -INFINITY, l = 0.f;
+    const float scl = a.scale * kLog2e;
+
+    Tile<T, S, D, RW, TK> tile;
+    const int kbeg = i0 * IK + grp * TK;
+    // the group's tiles: keys kbeg + j * IK, j < nj (as many rounds for every group)
+    const int nj = end > i0 * IK ? min(ni, (end - i0 * IK + IK - 1) / IK) : 0;
+    auto has = [&](int j) { return j < nj && kbeg + j * IK < end; };
+    if (has(0)) {
+      tile.pages(c, table, kbeg, end, tg);
+      tile.load(c, hk, kbeg, end, tg);
+    }
+    if (has(1)) tile.pages(c, table, kbeg + IK, end, tg);
+    for (int j = 0; j < nj; ++j) {
+      const int k0 = kbeg + j * IK;
+      const bool live = has(j);
+      const bool masked = k0 + TK > vis_all;
+      unsigned char *kb = buf + (Sh::NBUF == 2 ? (j & 1) * Sh::BUF : 0);
+      uint32_t odd = 0;
+      if (live) {
+        odd = __builtin_amdgcn_ballot_w64(tile.store(kb, tg, end - k0, masked)) != 0;
+        if (RW > 1 && lane == 0) s_odd[j & 1][wave] = odd;
+      }
+      if (has(j + 1)) tile.load(c, hk, k0 + IK, end, tg);
+      if (has(j + 2)) tile.pages(c, table, k0 + 2 * IK, end, tg);
+      if constexpr (RW > 1) __syncthreads();
+      if (!live) continue;
+      const unsigned char *vb = kb + TK * Sh::RB;
+
+      // S^T = K Q^T: keys 32 sub + n32 as rows
+      f32x16 s[NS];
+#pragma unroll
+      for (int u = 0; u < NS; ++u) s[u] = f32x16(0.f);
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+        for (int u = 0; u < NS; ++u) {
+          const u32x4 kf = reinterpret_cast<const u32x4 *>(kb)[piece_at<VPR>(32 * u + n32, 2 * cc + h)];
+          if constexpr (sizeof(T) == 2) {
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                           __builtin_bit_cast(bf16x8, qf[cc]), s[u], 0, 0, 0);
+          } else {
+            const f32x4 ka = __builtin_bit_cast(f32x4, kf), qa = __builtin_bit_cast(f32x4, qf[cc]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(ka[w], qa[w], s[u], 0, 0, 0);
+          }
+        }
+      // register r of sub-tile u: key 32 u + 8 (r / 4) + 4 h + r % 4
+      uint32_t seen[NS];
+      if (masked) {
+#pragma unroll
+        for (int u = 0; u < NS; ++u) {
+          seen[u] = 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = k0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4, cn = key - sp.P;
+            bool vis = cn < 0;
+            if (cn >= 0 && cn < sp.n)
+              vis = a.mask ? a.mask[((size_t)b * a.T + node) * a.T + cn] != 0 : cn <= node;
+            seen[u] |= (uint32_t)vis << r;
+            s[u][r] = vis ? s[u][r] : -INFINITY;
+          }
+        }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
+      mx = xor32_max(mx) * scl;
+      // the maximum is raised only when a score passes it by 2^8: probabilities
+      // stay below that, and the accumulators are seldom rescaled
+      const bool up = mx > m + kLazyMax;
+      if (__builtin_amdgcn_ballot_w64(up)) {
+        const float mn = up ? mx : m;
+        const float alpha = sexp2(m, mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+      }
+      const float mr = m == -INFINITY ? 0.f : m;  // no key seen yet
+      uint32_t pw[NS][sizeof(T) == 2 ? 8 : 16];   // probabilities, as the product takes them
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(s[u][r] * scl - mr);
+          const float p1 = __builtin_amdgcn_exp2f(s[u][r + 1] * scl - mr);
+          if constexpr (sizeof(T) == 2) {
+            // the sum takes the rounded values, so the result is a weighted mean
+            pw[u][r / 2] = f2bf2(p0, p1);
+            l += __uint_as_float(pw[u][r / 2] << 16) + __uint_as_float(pw[u][r / 2] & 0xffff0000u);
+          } else {
+            pw[u][r] = __float_as_uint(p0);
+            pw[u][r + 1] = __float_as_uint(p1);
+            l += p0 + p1;
+          }
+        }
+      if (masked) {
+        if constexpr (RW > 1) {
+#pragma unroll
+          for (int w = 0; w < RW; ++w) odd |= s_odd[j & 1][grp * RW + w];
+        }
+        if (odd) {
+          // a value row that some row does not see may hold an infinity or NaN:
+          // key by key, every row over the keys it sees
+#pragma unroll 1
+          for (int key = 0; key < TK; ++key) {
+            const int u0 = key >> 5, r0 = (key >> 3 & 3) * 4 + (key & 3), from = n32 + 32 * (key >> 2 & 1);
+            uint32_t w = 0, sn = 0;
+#pragma unroll
+            for (int u = 0; u < NS; ++u)
+              if (u == u0) {
+                sn = seen[u];
+#pragma unroll
+                for (int r = 0; r < (sizeof(T) == 2 ? 8 : 16); ++r)
+                  if (r == (sizeof(T) == 2 ? r0 / 2 : r0)) w = pw[u][r];
+              }
+            w = __shfl(w, from, 64);
+            sn = __shfl(sn, from, 64);
+            const float p = sizeof(T) == 4 ? __uint_as_float(w)
+                                           : __uint_as_float((r0 & 1) ? w & 0xffff0000u : w << 16);
+            const bool vis = sn >> r0 & 1;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+              for (int g8 = 0; g8 < 4; ++g8) {
+                const int d0 = 32 * dt + 8 * g8 + 4 * h, by = d0 * (int)sizeof(T);
+                const T *vp = reinterpret_cast<const T *>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
+#pragma unroll
+                for (int w4 = 0; w4 < 4; ++w4)
+                  if (vis) o[dt][4 * g8 + w4] += p * Elt<T>::to_f(vp[w4]);
+              }
+          }
+          continue;
+        }
+      }
+      // O^T += V^T P^T over the tile's keys
+#pragma unroll
+      for (int u = 0; u < NS; ++u) {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const u32x4 pf = {pw[u][2 * i], pw[u][2 * i + 1], pw[u][2 * i + 2], pw[u][2 * i + 3]};
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) {
+              // keys 8 i + 4 h + 0 .. 3 and the same 8 further, dim 32 dt + n32: the
+              // transposing read (lane 4 e + q of 16 names key e, dims 4 q .. + 3)
+              const int R = 32 * u + 8 * i + 4 * h + (lane >> 2 & 3);
+              const int p = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+              auto tr = [&](int key) {
+                return __builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(
+                               vb + 16 * piece_at<VPR>(key, p) + 8 * (lane & 1))));
+              };
+              const u32x2 v0 = tr(R), v1 = tr(R + 8);
+              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  __builtin_bit_cast(bf16x8, (u32x4{v0.x, v0.y, v1.x, v1.y})), __builtin_bit_cast(bf16x8, pf),
+                  o[dt], 0, 0, 0);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = 32 * u + 8 * (r / 4) + 4 * h + r % 4;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) {
+              const int by = 4 * (32 * dt + n32);
+              const float vf = *reinterpret_cast<const float *>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
+              o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, __uint_as_float(pw[u][r]), o[dt], 0, 0, 0);
+            }
+          }
+        }
+      }
+    }
+    l = xor32_sum(l);
+
+    // groups add up: group g > 0 leaves its sums in LDS, group 0 takes them in order
+    if constexpr (KW > 1) {
+      f32x4 *so = reinterpret_cast<f32x4 *>(s_mem);  // [(KW - 1) RW][D / 8][64]
+      static_assert((KW - 1) * RW * (D / 8) * 64 * 16 <= Sh::LDS, "sums fit the tiles' buffers");
+      __syncthreads();
+      if (grp > 0) {
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int g8 = 0; g8 < 4; ++g8)
+            so[(((grp - 1) * RW + rw) * (D / 8) + 4 * dt + g8) * 64 + lane] =
+                f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
+        s_ml[wave * 64 + lane][0] = m;
+        s_ml[wave * 64 + lane][1] = l;
+      }
+      __syncthreads();
+      if (grp == 0) {
+        float mm = m;
+#pragma unroll
+        for (int g = 1; g < KW; ++g) mm = fmaxf(mm, s_ml[(g * RW + rw) * 64 + lane][0]);
+        const float sc0 = sexp2(m, mm);
+        l *= sc0;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[dt] *= sc0;
+#pragma unroll
+        for (int g = 1; g < KW; ++g) {
+          const float scg = sexp2(s_ml[(g * RW + rw) * 64 + lane][0], mm);
+          l += s_ml[(g * RW + rw) * 64 + lane][1] * scg;
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+            for (int g8 = 0; g8 < 4; ++g8) {
+              const f32x4 w = so[(((g - 1) * RW + rw) * (D / 8) + 4 * dt + g8) * 64 + lane];
+#pragma unroll
+              for (int w4 = 0; w4 < 4; ++w4) o[dt][4 * g8 + w4] += w[w4] * scg;
+            }
+        }
+        m = mm;
+      }
+    }
+    if (grp == 0 && row < sp.live) {
+      const bool head_cut = i0 > 0, whole = ni == it;
+      if (whole) {
+        const float inv = sp.bad ? __int_as_float(0x7fc00000) : l == 0.f ? 0.f : 1.f / l;
+        T *op = (T *)a.out + (((long)b * a.T + node) * a.Hq + head) * D + 4 * h;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int g8 = 0; g8 < 4; ++g8) {
+            const f32x4 w = f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]} * inv;
+            if constexpr (sizeof(T) == 2)
+              *reinterpret_cast<u32x2 *>(op + 32 * dt + 8 * g8) = u32x2{f2bf2(w.x, w.y), f2bf2(w.z, w.w)};
+            else
+              *reinterpret_cast<f32x4 *>(op + 32 * dt + 8 * g8) = w;
+          }
+      } else {
+        const long slot = 2L * wg + (head_cut ? 0 : 1);
+        const int rr = 32 * rw + n32;
+        float *po = work.o(slot) + (long)rr * D + 4 * h;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int g8 = 0; g8 < 4; ++g8)
+            *reinterpret_cast<f32x4 *>(po + 32 * dt + 8 * g8) =
+                f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
+        if (h == 0) *reinterpret_cast<float2 *>(work.ml(slot) + 2 * rr) = float2{m, l};
+      }
+    }
+    __syncthreads();  // LDS is free for the next segment
+  }
 }
 
-template <typename T, typename S>
-hipError_t rows_t(const TreeArgs &a, hipStream_t s) {
-  const long waves = (long)a.B * a.T * a.Hq;
-  if (a.c.D == 64)
-    k_tree_attn_rows<T, S, 64><<<(waves + 3) / 4, 256, 0, s>>>(a);
+// Joins the partials of one segment in the order of their ranges: a workgroup per
+// (sequence, row tile, KV head) and 1024 / D rows, four dims a thread.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int nrt, int W_, int TR) {
+  constexpr int RPW = 1024 / D;
+  const PagedView &c = a.c;
+  const Work<D> work{a.ws, 2L * W_, TR};
+  const int E = a.B * nrt, e = blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv;
+  const long before = work.before()[e], it = work.before()[e + 1] - before;
+  if (it == 0) return;
+  const Ranges rg(work.before()[E] * c.Hkv, W_);
+  const long S = before * c.Hkv + hk * it;
+  const long w0 = rg.owner(S), w1 = rg.owner(S + it - 1);
+  if (w0 == w1) return;  // one range held it all and wrote the rows
+  const Span sp = span_of(a, e / nrt);
+  const int rr = blockIdx.y * RPW + threadIdx.x / (D / 4), d0 = 4 * (threadIdx.x % (D / 4));
+  const int row = (e % nrt) * TR + rr;
+  if (rr >= TR || row >= sp.live) return;
+  auto slot = [&](long w) { return w == w0 ? 2 * w + 1 : 2 * w; };
+  float M = -INFINITY;
+  for (long w = w0; w <= w1; ++w) M = fmaxf(M, work.ml(slot(w))[2 * rr]);
+  float L = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (long w = w0; w <= w1; ++w) {
+    const float2 ml = *reinterpret_cast<const float2 *>(work.ml(slot(w)) + 2 * rr);
+    const float sc = sexp2(ml.x, M);
+    L += ml.y * sc;
+    o += *reinterpret_cast<const f32x4 *>(work.o(slot(w)) + (long)rr * D + d0) * sc;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  o *= inv;
+  const int G = a.Hq / c.Hkv;
+  T *op = (T *)a.out + (((long)(e / nrt) * a.T + row / G) * a.Hq + hk * G + row % G) * D + d0;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2 *>(op) = u32x2{f2bf2(o.x, o.y), f2bf2(o.z, o.w)};
   else
-    k_tree_attn_rows<T, S, 128><<<(waves + 3) / 4, 256, 0, s>>>(a);
+    *reinterpret_cast<f32x4 *>(op) = o;
+}
+
+// ---- host ---------------------------------------------------------------------------
+
+// Compute units of the current device (asked once per device).
+int compute_units() {
+  static std::atomic<int> known[64];
+  int d = 0;
+  if (hipGetDevice(&d) != hipSuccess || d < 0 || d >= 64) return 256;
+  int n = known[d].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, d) != hipSuccess || n <= 0) n = 256;
+    known[d].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// The launch of a call: rows per tile, keys per work item, row tiles per sequence,
+// ranges, and whether a segment may be cut at all.
+struct Plan {
+  int RW, KW, nrt, W;
+  bool join;
+};
+
+// Workgroups: two per compute unit, no more than there can be work items.
+constexpr int kWgPerCu = 2;
+constexpr int kMaxCus = 512;
+
+Plan plan_of(const PagedView &c, int B, int T, int Hq, int cus) {
+  const int rows = T * (Hq / c.Hkv);
+  Plan p;
+  p.RW = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  p.KW = 4 / p.RW;
+  const int TR = 32 * p.RW, IK = p.RW == 1 ? 128 : 64;
+  p.nrt = (rows + TR - 1) / TR;
+  const long most = ((long)c.max_len + IK - 1) / IK;
+  const long items = (long)B * p.nrt * c.Hkv * most;
+  p.W = (int)std::min<long>(items, (long)kWgPerCu * cus);
+  p.join = most > 1 && p.W > 0;
+  return p;
+}
+
+template <typename T, typename S, int D, int RW, int KW>
+hipError_t launch(const TreeArgs &a, const Plan &p, hipStream_t s) {
+  k_tree_attn<T, S, D, RW, KW><<<p.W, 64 * RW * KW, 0, s>>>(a, p.nrt, p.W);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.join) return e;
+  constexpr int TR = 32 * RW;
+  const int rows = std::min<long>(TR, (long)a.T * (a.Hq / a.c.Hkv));
+  k_tree_join<T, D><<<dim3(a.B * p.nrt * a.c.Hkv, (rows * D + 1023) / 1024), 256, 0, s>>>(a, p.nrt, p.W, TR);
   return hipGetLastError();
+}
+
+template <typename T, typename S, int D> hipError_t by_rows(const TreeArgs &a, const Plan &p, hipStream_t s) {
+  return p.RW == 1 ? launch<T, S, D, 1, 4>(a, p, s)
+         : p.RW == 2 ? launch<T, S, D, 2, 2>(a, p, s)
+                     : launch<T, S, D, 4, 1>(a, p, s);
+}
+
+template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Plan &p, hipStream_t s) {
+  return a.c.D == 64 ? by_rows<T, S, 64>(a, p, s) : by_rows<T, S, 128>(a, p, s);
 }
 
 }  // namespace
 
-size_t tree_attention_ws(const PagedView &, int, int, int, int) { return 256; }
+size_t tree_attention_ws(const PagedView &c, int B, int T, int Hq, int) {
+  const Plan p = plan_of(c, B, T, Hq, kMaxCus);
+  const size_t rows = 2 * (size_t)p.W * 32 * p.RW;
+  return (rows * (c.D + 2) * 4 + ((size_t)B * p.nrt + 1) * 8 + 255) & ~(size_t)255;
+}
 
 hipError_t tree_attention(const TreeArgs &a, int dt, hipStream_t s) {
-  if (dt == kF32) return a.c.dtype == kF8 ? rows_t<float, uint8_t>(a, s) : rows_t<float, float>(a, s);
-  return a.c.dtype == kF8 ? rows_t<uint16_t, uint8_t>(a, s) : rows_t<uint16_t, uint16_t>(a, s);
+  const Plan p = plan_of(a.c, a.B, a.T, a.Hq, std::min(compute_units(), kMaxCus));
+  if (dt == kF32) return a.c.dtype == kF8 ? by_dim<float, uint8_t>(a, p, s) : by_dim<float, float>(a, p, s);
+  return a.c.dtype == kF8 ? by_dim<uint16_t, uint8_t>(a, p, s) : by_dim<uint16_t, uint16_t>(a, p, s);
 }
 
 }  // namespace fe
