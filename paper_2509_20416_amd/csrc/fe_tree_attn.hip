@@ -29,6 +29,7 @@
 //    holds one is added key by key, each row over the keys it sees.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "fe_attn_unit.h"
 #include "fe_paged.h"
@@ -86,11 +87,12 @@ __device__ __forceinline__ int items_of(const TreeArgs &a, int e, int nrt, int T
   return max(1, (keys_end(a, s, rt, TR) + IK - 1) / IK);
 }
 
-__device__ __forceinline__ long wave_incl_scan(long x) {
+// Sums of a wave's values up to each lane (below 2^32: an item count is at most 2^25).
+__device__ __forceinline__ uint32_t wave_incl_scan(uint32_t x) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const long y = __shfl_up(x, o, 64);
+    const uint32_t y = __shfl_up(x, o, 64);
     if (lane >= o) x += y;
   }
   return x;
@@ -101,10 +103,14 @@ __device__ __forceinline__ long wave_incl_scan(long x) {
 struct Ranges {
   long total, W;
   __device__ __forceinline__ Ranges(long items, int wgs) : total(items), W(items < wgs ? items : wgs) {}
-  __device__ __forceinline__ long begin(long w) const { return total * w / W; }
+  // products below 2^32 are the rule, and a 64-bit division costs 4 times theirs
+  __device__ __forceinline__ static long div(long x, long y) {
+    return (x | y) >> 32 ? x / y : (long)((uint32_t)x / (uint32_t)y);
+  }
+  __device__ __forceinline__ long begin(long w) const { return div(total * w, W); }
   // the range that holds item x
   __device__ __forceinline__ long owner(long x) const {
-    const long w = ((x + 1) * W + total - 1) / total - 1;
+    const long w = div((x + 1) * W + total - 1, total) - 1;
     return w < W - 1 ? w : W - 1;
   }
 };
@@ -230,8 +236,30 @@ template <typename T, typename S, int D, int RW, int TK> struct Tile {
 
 // ---- the kernel -------------------------------------------------------------------
 
+// A value the compiler cannot compute ahead of a seldom taken branch, so that the
+// branch's addresses hold no registers outside it.
+template <typename V> __device__ __forceinline__ V opaque(V x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Bytes c .. c + 3 of a mask row of T: one (unaligned) load where T >= 4, moved
+// inside the row and shifted back; bytes outside the row are 0.
+__device__ __forceinline__ uint32_t mask_word(const uint8_t *mp, int c, int T) {
+  uint32_t w = 0;
+  int at = 0;
+  if (T >= 4) {
+    at = min(max(c, 0), T - 4);
+    __builtin_memcpy(&w, mp + at, 4);
+  } else {
+    for (int i = 0; i < T; ++i) w |= (uint32_t)mp[i] << 8 * i;
+  }
+  const int d = c - at;
+  return d >= 4 || d <= -4 ? 0u : d >= 0 ? w >> 8 * d : w << -8 * d;
+}
+
 template <typename T, typename S, int D, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt, int W_) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
   using Sh = Shape<T, D, RW, KW>;
   constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / 32;
   constexpr int VPR = D * (int)sizeof(T) / 16;
@@ -248,19 +276,21 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
   const int G = a.Hq / c.Hkv, E = a.B * nrt;
   // the items of every segment, this range of them, and the segment it starts in
   Work<D> work{a.ws, 2L * W_, TR};
-  long total = 0;
+  long total = 0, before = 0;
+  uint32_t mine = 0;
   for (int e0 = 0; e0 < E; e0 += NT) {
-    const long x = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
-    const long inc = wave_incl_scan(x);
+    mine = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
+    const uint32_t inc = wave_incl_scan(mine);
     if (lane == 63) s_scan[wave] = inc;
     __syncthreads();
-    long base = total;
+    before = total + inc - mine;
+#pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-      if (w < wave) base += s_scan[w];
+      if (w < wave) before += s_scan[w];
       total += s_scan[w];
     }
-    if (blockIdx.x == 0 && e0 + tid < E) work.before()[e0 + tid] = base + inc - x;
-    __syncthreads();
+    if (blockIdx.x == 0 && e0 + tid < E) work.before()[e0 + tid] = before;
+    if (e0 + NT < E) __syncthreads();
   }
   if (blockIdx.x == 0 && tid == 0) work.before()[E] = total;
   const Ranges rg(total * c.Hkv, W_);
@@ -268,26 +298,34 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
   // neighbouring ranges on one XCD: workgroups go round the 8 of them
   const int xcd = blockIdx.x % 8, wg = (int)(xcd * (rg.W / 8) + min((long)xcd, rg.W % 8)) + blockIdx.x / 8;
   const long x0 = rg.begin(wg), x1 = rg.begin(wg + 1);
-  {
+  auto find = [&](int e0) {
+    const long lo = before * c.Hkv;
+    if (mine > 0 && lo <= x0 && x0 < lo + (long)mine * c.Hkv) {
+      s_first[0] = e0 + tid;
+      s_first[1] = lo;
+    }
+  };
+  if (E <= NT) {
+    find(0);
+    __syncthreads();
+  } else {  // a second walk: the first kept only its last stretch
     long run = 0;
     for (int e0 = 0; e0 < E; e0 += NT) {
-      const long x = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
-      const long inc = wave_incl_scan(x);
+      __syncthreads();
+      mine = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
+      const uint32_t inc = wave_incl_scan(mine);
       if (lane == 63) s_scan[wave] = inc;
       __syncthreads();
-      long base = run;
+      before = run + inc - mine;
+#pragma unroll
       for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) base += s_scan[w];
+        if (w < wave) before += s_scan[w];
         run += s_scan[w];
       }
-      const long lo = (base + inc - x) * c.Hkv;
-      if (x > 0 && lo <= x0 && x0 < lo + x * c.Hkv) {
-        s_first[0] = e0 + tid;
-        s_first[1] = lo;
-      }
-      __syncthreads();
+      find(e0);
       if (run * c.Hkv > x0) break;
     }
+    __syncthreads();
   }
   int e = (int)s_first[0];
   long at = s_first[1];  // first item of entry e
@@ -308,7 +346,7 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
     // this lane's row: node, head
     const int row = rt * TR + 32 * rw + n32, rowc = min(row, sp.live - 1);
     const int node = rowc / G, head = hk * G + rowc % G;
-    const int vis_all = sp.P + (a.mask ? 0 : rt * TR / G + 1);  // keys every row sees
+    const int vis_all = sp.bad ? 0 : sp.P + (a.mask ? 0 : rt * TR / G + 1);  // keys every row sees
     const int32_t *table = c.pages + (size_t)b * c.max_pages;
 
     // q, 16 bytes of two neighbouring pieces per step: the right operand
@@ -334,10 +372,11 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
       tile.load(c, hk, kbeg, end, tg);
     }
     if (has(1)) tile.pages(c, table, kbeg + IK, end, tg);
-    for (int j = 0; j < nj; ++j) {
+    // tile j; kMasked: some row may not see all of it (the last tiles)
+    auto step = [&](int j, auto kMasked) {
+      constexpr bool masked = decltype(kMasked)::value;
       const int k0 = kbeg + j * IK;
-      const bool live = has(j);
-      const bool masked = k0 + TK > vis_all;
+      const bool live = !masked || has(j);
       unsigned char *kb = buf + (Sh::NBUF == 2 ? (j & 1) * Sh::BUF : 0);
       uint32_t odd = 0;
       if (live) {
@@ -347,7 +386,7 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
       if (has(j + 1)) tile.load(c, hk, k0 + IK, end, tg);
       if (has(j + 2)) tile.pages(c, table, k0 + 2 * IK, end, tg);
       if constexpr (RW > 1) __syncthreads();
-      if (!live) continue;
+      if (!live) return;
       const unsigned char *vb = kb + TK * Sh::RB;
 
       // S^T = K Q^T: keys 32 sub + n32 as rows
@@ -369,28 +408,36 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
           }
         }
       // register r of sub-tile u: key 32 u + 8 (r / 4) + 4 h + r % 4
-      uint32_t seen[NS];
-      if (masked) {
+      [[maybe_unused]] uint32_t seen[NS];  // bit r: register r's key is seen
+      if constexpr (masked) {
+        const uint8_t *mp = opaque(a.mask ? a.mask + ((size_t)b * a.T + node) * a.T : nullptr);
+        const int c0 = opaque(k0 - sp.P + 4 * h);
 #pragma unroll
         for (int u = 0; u < NS; ++u) {
           seen[u] = 0;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = k0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4, cn = key - sp.P;
-            bool vis = cn < 0;
-            if (cn >= 0 && cn < sp.n)
-              vis = a.mask ? a.mask[((size_t)b * a.T + node) * a.T + cn] != 0 : cn <= node;
-            seen[u] |= (uint32_t)vis << r;
-            s[u][r] = vis ? s[u][r] : -INFINITY;
+          for (int i = 0; i < 4; ++i) {  // four neighbouring keys
+            const int cn = c0 + 32 * u + 8 * i;
+            const uint32_t own = mp ? mask_word(mp, cn, a.T) : 0u;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const uint32_t in_mask = mp ? (own >> 8 * v & 255) != 0 : cn + v <= node;
+              const uint32_t inside = cn + v < sp.n;
+              seen[u] |= ((uint32_t)(cn + v < 0) | (inside & in_mask)) << (4 * i + v);
+            }
           }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = (seen[u] >> r & 1) ? s[u][r] : -INFINITY;
         }
       }
-      float mx = s[0][0];
+      float mx = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < NS; ++u)
+      for (int u = 0; u < NS; ++u) {
+        s[u] *= scl;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
-      mx = xor32_max(mx) * scl;
+        for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[u][r]), s[u][r + 1]);
+      }
+      mx = xor32_max(mx);
       // the maximum is raised only when a score passes it by 2^8: probabilities
       // stay below that, and the accumulators are seldom rescaled
       const bool up = mx > m + kLazyMax;
@@ -408,19 +455,20 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
       for (int u = 0; u < NS; ++u)
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(s[u][r] * scl - mr);
-          const float p1 = __builtin_amdgcn_exp2f(s[u][r + 1] * scl - mr);
+          const float p0 = __builtin_amdgcn_exp2f(s[u][r] - mr);
+          const float p1 = __builtin_amdgcn_exp2f(s[u][r + 1] - mr);
           if constexpr (sizeof(T) == 2) {
             // the sum takes the rounded values, so the result is a weighted mean
             pw[u][r / 2] = f2bf2(p0, p1);
-            l += __uint_as_float(pw[u][r / 2] << 16) + __uint_as_float(pw[u][r / 2] & 0xffff0000u);
+            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[u][r / 2]),
+                                                __builtin_bit_cast(bf16x2_t, 0x3f803f80u), l, false);
           } else {
             pw[u][r] = __float_as_uint(p0);
             pw[u][r + 1] = __float_as_uint(p1);
             l += p0 + p1;
           }
         }
-      if (masked) {
+      if constexpr (masked) {
         if constexpr (RW > 1) {
 #pragma unroll
           for (int w = 0; w < RW; ++w) odd |= s_odd[j & 1][grp * RW + w];
@@ -430,6 +478,7 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
           // key by key, every row over the keys it sees
 #pragma unroll 1
           for (int key = 0; key < TK; ++key) {
+            const int hh = opaque(h);
             const int u0 = key >> 5, r0 = (key >> 3 & 3) * 4 + (key & 3), from = n32 + 32 * (key >> 2 & 1);
             uint32_t w = 0, sn = 0;
 #pragma unroll
@@ -449,14 +498,14 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
             for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
               for (int g8 = 0; g8 < 4; ++g8) {
-                const int d0 = 32 * dt + 8 * g8 + 4 * h, by = d0 * (int)sizeof(T);
+                const int d0 = 32 * dt + 8 * g8 + 4 * hh, by = d0 * (int)sizeof(T);
                 const T *vp = reinterpret_cast<const T *>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
 #pragma unroll
                 for (int w4 = 0; w4 < 4; ++w4)
                   if (vis) o[dt][4 * g8 + w4] += p * Elt<T>::to_f(vp[w4]);
               }
           }
-          continue;
+          return;
         }
       }
       // O^T += V^T P^T over the tile's keys
@@ -496,7 +545,13 @@ __global__ __launch_bounds__(64 * RW * KW) void k_tree_attn(TreeArgs a, int nrt,
           }
         }
       }
-    }
+    };
+    const int room = vis_all - TK - kbeg;  // the first tile that is masked starts behind it
+    const int jm = room < 0 ? 0 : min(nj, room / IK + 1);
+#pragma unroll 1
+    for (int j = 0; j < jm; ++j) step(j, std::false_type{});
+#pragma unroll 1
+    for (int j = jm; j < nj; ++j) step(j, std::true_type{});
     l = xor32_sum(l);
 
     // groups add up: group g > 0 leaves its sums in LDS, group 0 takes them in order
@@ -590,16 +645,35 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int nrt, int W_, 
   const int row = (e % nrt) * TR + rr;
   if (rr >= TR || row >= sp.live) return;
   auto slot = [&](long w) { return w == w0 ? 2 * w + 1 : 2 * w; };
+  // the row's D / 4 lanes hold a partial's maximum and sum each, then take turns
+  // handing out the weights
+  constexpr int GL = D / 4;
+  const int gl = threadIdx.x % GL;
   float M = -INFINITY;
-  for (long w = w0; w <= w1; ++w) M = fmaxf(M, work.ml(slot(w))[2 * rr]);
+  for (long w = w0; w <= w1; w += GL)
+    if (w + gl <= w1) M = fmaxf(M, work.ml(slot(w + gl))[2 * rr]);
+  M = group_max<GL>(M);
   float L = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (long w = w0; w <= w1; ++w) {
-    const float2 ml = *reinterpret_cast<const float2 *>(work.ml(slot(w)) + 2 * rr);
+  for (long w = w0; w <= w1; w += GL) {
+    const int n = (int)min((long)GL, w1 + 1 - w);
+    float2 ml = {-INFINITY, 0.f};
+    if (gl < n) ml = *reinterpret_cast<const float2 *>(work.ml(slot(w + gl)) + 2 * rr);
     const float sc = sexp2(ml.x, M);
     L += ml.y * sc;
-    o += *reinterpret_cast<const f32x4 *>(work.o(slot(w)) + (long)rr * D + d0) * sc;
+    for (int i = 0; i < n; i += 8) {
+      f32x4 part[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        part[u] = *reinterpret_cast<const f32x4 *>(work.o(slot(w + min(i + u, n - 1))) + (long)rr * D + d0);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float su = __shfl(sc, min(i + u, GL - 1), GL);
+        if (i + u < n) o += part[u] * su;
+      }
+    }
   }
+  L = group_sum<GL>(L);
   const float inv = L == 0.f ? 0.f : 1.f / L;
   o *= inv;
   const int G = a.Hq / c.Hkv;
