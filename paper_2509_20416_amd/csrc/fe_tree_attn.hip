@@ -127,6 +127,11 @@ template <int D> struct Work {
   __host__ __device__ long *before() const { return (long *)(p + slots * TR * (D + 2)); }
 };
 
+// Two of a word's e4m3 codes, times a power of two, as bf16 (exact).
+template <bool HI> __device__ __forceinline__ uint32_t f8_bf16(uint32_t w, float sc) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, HI));
+}
+
 // ---- one tile of keys: global memory -> registers -> LDS ---------------------------
 
 // 16-byte piece p of row R (rows of VPR pieces) in LDS: pieces are permuted within
@@ -139,45 +144,63 @@ template <int VPR> __device__ __forceinline__ int piece_at(int R, int p) {
     return R * VPR + (p ^ (((R & 3) << 2) | ((R >> 2) & 3)));
 }
 
-template <typename T, typename S, int D, int RW, int TK> struct Tile {
+// A wave's rows in one load are at most 16 neighbours (and a page holds whole runs
+// of 16), so the page and the row's address are wave-uniform: the ids of the next
+// 1024 keys' pages sit in one register, a lane per 16 keys, and each load picks its
+// own with a readlane.
+template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
   static constexpr int PS = D * (int)sizeof(S) / 16;  // 16-byte pieces of a stored row
   static constexpr int VPR = D * (int)sizeof(T) / 16;
-  static constexpr int STEP = 64 * RW / PS;           // rows between a thread's loads
+  static constexpr int SPAN = 64 / PS;                // rows of one load of a wave
+  static constexpr int STEP = RW * SPAN;              // rows between a thread's loads
   static constexpr int NL = TK / STEP;                // loads per thread, K (as many V)
-  static_assert(STEP >= 1 && NL >= 1 && TK % STEP == 0, "whole loads");
-  static constexpr int NP = STEP >= 16 ? NL : TK / 16;  // pages per thread: rows of one page share it
+  static_assert(SPAN >= 1 && SPAN <= 16 && NL >= 1 && TK % STEP == 0, "whole loads inside runs of 16 rows");
+  static constexpr int WIN = 1024 / IK;               // tiles per register of page ids
   static constexpr bool F8 = sizeof(S) == 1;
   u32x4 k[NL], v[NL];
   uint32_t sk[NL], sv[NL];  // scale bytes
-  int pid[NP];
-  uint32_t badp;  // bit i: load i's page lies outside the pool
+  int pid, pid_next;        // lane l: page of keys 16 l .. + 15 of this window, of the next
+  uint32_t badp;            // bit i: load i's page lies outside the pool
+  int rw, lrow, lpc;        // this wave; this lane's row and piece in its load
+  uint32_t loff;
 
-  __device__ __forceinline__ int row(int i, int tg) const { return i * STEP + tg / PS; }
-
-  __device__ __forceinline__ void pages(const PagedView &c, const int32_t *table, int k0, int end, int tg) {
-#pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int R = STEP >= 16 ? row(j, tg) : 16 * j + tg / PS;
-      pid[j] = table[min(k0 + R, end - 1) >> c.shift];
-    }
+  __device__ __forceinline__ void init(const PagedView &c, int rw_, int lane) {
+    rw = rw_;
+    lrow = lane / PS;
+    lpc = lane % PS;
+    loff = lrow * (uint32_t)(c.Hkv * D * sizeof(S)) + 16 * lpc;
   }
-  // `pages` has run for the same k0.  Rows past end are loaded clamped.
-  __device__ __forceinline__ void load(const PagedView &c, int hk, int k0, int end, int tg) {
+  __device__ __forceinline__ int row(int i) const { return i * STEP + rw * SPAN + lrow; }
+  __device__ __forceinline__ static int ids(const PagedView &c, const int32_t *table, int w0, int end) {
+    return table[min(w0 + 16 * (int)(threadIdx.x & 63), end - 1) >> c.shift];
+  }
+  // The first two windows of a run of tiles that starts at key k0.
+  __device__ __forceinline__ void pages(const PagedView &c, const int32_t *table, int k0, int end) {
+    pid = ids(c, table, k0, end);
+    pid_next = ids(c, table, min(k0 + 1024, end), end);
+  }
+  // Loads tile j of the run (keys k0 ..); rows past end are some row of a page
+  // that belongs to the sequence.
+  __device__ __forceinline__ void load(const PagedView &c, const int32_t *table, int hk, int j, int k0, int end) {
+    if (j > 0 && j % WIN == 0) {
+      pid = pid_next;
+      pid_next = ids(c, table, min(k0 + 1024, end), end);
+    }
     badp = 0;
-    const long rowb = (long)c.Hkv * D * sizeof(S);
-    const int off = hk * D * (int)sizeof(S) + 16 * (tg % PS);
+    const uint32_t rowb = c.Hkv * D * sizeof(S);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int pos = min(k0 + row(i, tg), end - 1);
-      const int pg = pid[STEP >= 16 ? i : i * STEP / 16];
+      const int R0 = i * STEP + rw * SPAN;  // uniform
+      const int pg = __builtin_amdgcn_readlane(pid, (j % WIN * IK + R0) / 16);
       const bool ok = (unsigned)pg < (unsigned)c.n_pages;
       if (!ok) badp |= 1u << i;
-      const long r = ((long)(ok ? pg : 0) << c.shift) + (pos & ((1 << c.shift) - 1));
-      k[i] = *reinterpret_cast<const u32x4 *>((const char *)c.k + r * rowb + off);
-      v[i] = *reinterpret_cast<const u32x4 *>((const char *)c.v + r * rowb + off);
+      const long r = ((long)(ok ? pg : 0) << c.shift) + ((k0 + R0) & ((1 << c.shift) - 1));
+      const long at = r * rowb + hk * (D * (int)sizeof(S));
+      k[i] = *reinterpret_cast<const u32x4 *>((const char *)c.k + at + loff);
+      v[i] = *reinterpret_cast<const u32x4 *>((const char *)c.v + at + loff);
       if constexpr (F8) {
-        sk[i] = c.ks[hk * c.rows() + r];
-        sv[i] = c.vs[hk * c.rows() + r];
+        sk[i] = (c.ks + hk * c.rows() + r)[(uint32_t)lrow];
+        sv[i] = (c.vs + hk * c.rows() + r)[(uint32_t)lrow];
       }
     }
   }
@@ -189,12 +212,13 @@ template <typename T, typename S, int D, int RW, int TK> struct Tile {
       const float sc = scale_of(s);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const f32x4 a = f8x4_to_f(w[2 * q]) * sc, b = f8x4_to_f(w[2 * q + 1]) * sc;
+        const uint32_t a = w[2 * q], b = w[2 * q + 1];
         if constexpr (sizeof(T) == 2) {
-          dst[piece_at<VPR>(R, 2 * p + q)] = u32x4{f2bf2(a.x, a.y), f2bf2(a.z, a.w), f2bf2(b.x, b.y), f2bf2(b.z, b.w)};
+          dst[piece_at<VPR>(R, 2 * p + q)] = u32x4{f8_bf16<false>(a, sc), f8_bf16<true>(a, sc),
+                                                   f8_bf16<false>(b, sc), f8_bf16<true>(b, sc)};
         } else {
-          dst[piece_at<VPR>(R, 4 * p + 2 * q)] = __builtin_bit_cast(u32x4, a);
-          dst[piece_at<VPR>(R, 4 * p + 2 * q + 1)] = __builtin_bit_cast(u32x4, b);
+          dst[piece_at<VPR>(R, 4 * p + 2 * q)] = __builtin_bit_cast(u32x4, f8x4_to_f(a) * sc);
+          dst[piece_at<VPR>(R, 4 * p + 2 * q + 1)] = __builtin_bit_cast(u32x4, f8x4_to_f(b) * sc);
         }
       }
     }
@@ -202,17 +226,17 @@ template <typename T, typename S, int D, int RW, int TK> struct Tile {
   // Writes the tile; ragged: rows from `left` on become zeros.  A row on a bad page
   // becomes NaN keys (and zero values).  Returns whether a value this thread wrote
   // is not finite (asked for masked tiles only).
-  __device__ __forceinline__ bool store(unsigned char *lds, int tg, int left, bool masked) {
+  template <bool masked> __device__ __forceinline__ bool store(unsigned char *lds, int left) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int R = row(i, tg);
+      const int R = row(i);
       u32x4 kw = k[i], vw = v[i];
       if (badp >> i & 1) {
         kw = u32x4(0xffffffffu);
         vw = u32x4(0u);
       }
-      if (masked) {
+      if constexpr (masked) {
         if (R >= left) kw = vw = u32x4(0u);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -227,8 +251,8 @@ template <typename T, typename S, int D, int RW, int TK> struct Tile {
           }
         }
       }
-      put(lds, R, tg % PS, kw, F8 ? sk[i] : 0);
-      put(lds + TK * D * sizeof(T), R, tg % PS, vw, F8 ? sv[i] : 0);
+      put(lds, R, lpc, kw, F8 ? sk[i] : 0);
+      put(lds + TK * D * sizeof(T), R, lpc, vw, F8 ? sv[i] : 0);
     }
     return odd;
   }
@@ -259,7 +283,7 @@ __device__ __forceinline__ uint32_t mask_word(const uint8_t *mp, int c, int T) {
 }
 
 template <typename T, typename S, int D, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
   using Sh = Shape<T, D, RW, KW>;
   constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / 32;
   constexpr int VPR = D * (int)sizeof(T) / 16;
@@ -270,8 +294,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_
   __shared__ long s_first[2];
   __shared__ uint32_t s_odd[2][RW * KW];
   const PagedView &c = a.c;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int grp = wave / RW, rw = wave % RW, tg = rw * 64 + lane;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int grp = wave / RW, rw = wave % RW;
   const int n32 = lane & 31, h = lane >> 5;
   const int G = a.Hq / c.Hkv, E = a.B * nrt;
   // the items of every segment, this range of them, and the segment it starts in
@@ -327,6 +351,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_
     }
     __syncthreads();
   }
+  Tile<T, S, D, RW, TK, IK> tile;
+  tile.init(c, rw, lane);
   int e = (int)s_first[0];
   long at = s_first[1];  // first item of entry e
   unsigned char *buf = s_mem + grp * Sh::NBUF * Sh::BUF;
@@ -359,19 +385,21 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_
     f32x16 o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x16(0.f);
+    // the running maximum in the scores' own units, and 16 copies of its negative
+    // that the first product starts from: scores come out relative to it
     float m = -INFINITY, l = 0.f;
-    const float scl = a.scale * kLog2e;
+    f32x16 base = f32x16(0.f);
+    const float scl = a.scale * kLog2e, inv_scl = 1.f / scl;
+    const bool wlive = rt * TR + 32 * rw < sp.live;  // some row of this wave is there
 
-    Tile<T, S, D, RW, TK> tile;
     const int kbeg = i0 * IK + grp * TK;
     // the group's tiles: keys kbeg + j * IK, j < nj (as many rounds for every group)
     const int nj = end > i0 * IK ? min(ni, (end - i0 * IK + IK - 1) / IK) : 0;
     auto has = [&](int j) { return j < nj && kbeg + j * IK < end; };
     if (has(0)) {
-      tile.pages(c, table, kbeg, end, tg);
-      tile.load(c, hk, kbeg, end, tg);
+      tile.pages(c, table, kbeg, end);
+      tile.load(c, table, hk, 0, kbeg, end);
     }
-    if (has(1)) tile.pages(c, table, kbeg + IK, end, tg);
     // tile j; kMasked: some row may not see all of it (the last tiles)
     auto step = [&](int j, auto kMasked) {
       constexpr bool masked = decltype(kMasked)::value;
@@ -380,19 +408,18 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_
       unsigned char *kb = buf + (Sh::NBUF == 2 ? (j & 1) * Sh::BUF : 0);
       uint32_t odd = 0;
       if (live) {
-        odd = __builtin_amdgcn_ballot_w64(tile.store(kb, tg, end - k0, masked)) != 0;
-        if (RW > 1 && lane == 0) s_odd[j & 1][wave] = odd;
+        odd = __builtin_amdgcn_ballot_w64(tile.template store<masked>(kb, end - k0)) != 0;
+        if (masked && RW > 1 && lane == 0) s_odd[j & 1][wave] = odd;
       }
-      if (has(j + 1)) tile.load(c, hk, k0 + IK, end, tg);
-      if (has(j + 2)) tile.pages(c, table, k0 + 2 * IK, end, tg);
+      if (has(j + 1)) tile.load(c, table, hk, j + 1, k0 + IK, end);
       if constexpr (RW > 1) __syncthreads();
-      if (!live) return;
+      if (!live || !wlive) return;
       const unsigned char *vb = kb + TK * Sh::RB;
 
       // S^T = K Q^T: keys 32 sub + n32 as rows
       f32x16 s[NS];
 #pragma unroll
-      for (int u = 0; u < NS; ++u) s[u] = f32x16(0.f);
+      for (int u = 0; u < NS; ++u) s[u] = base;
 #pragma unroll
       for (int cc = 0; cc < NC; ++cc)
 #pragma unroll
@@ -440,23 +467,24 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_
       mx = xor32_max(mx);
       // the maximum is raised only when a score passes it by 2^8: probabilities
       // stay below that, and the accumulators are seldom rescaled
-      const bool up = mx > m + kLazyMax;
+      const bool up = mx > (m == -INFINITY ? -INFINITY : kLazyMax);
       if (__builtin_amdgcn_ballot_w64(up)) {
-        const float mn = up ? mx : m;
-        const float alpha = sexp2(m, mn);
-        m = mn;
+        const float by = up ? mx : 0.f, alpha = __builtin_amdgcn_exp2f(-by);
+        if (up) m = (m == -INFINITY ? 0.f : m) + by * inv_scl;
+        base = f32x16(m == -INFINITY ? 0.f : -m);
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+#pragma unroll
+        for (int u = 0; u < NS; ++u) s[u] -= by;
       }
-      const float mr = m == -INFINITY ? 0.f : m;  // no key seen yet
       uint32_t pw[NS][sizeof(T) == 2 ? 8 : 16];   // probabilities, as the product takes them
 #pragma unroll
       for (int u = 0; u < NS; ++u)
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(s[u][r] - mr);
-          const float p1 = __builtin_amdgcn_exp2f(s[u][r + 1] - mr);
+          const float p0 = __builtin_amdgcn_exp2f(s[u][r]);
+          const float p1 = __builtin_amdgcn_exp2f(s[u][r + 1]);
           if constexpr (sizeof(T) == 2) {
             // the sum takes the rounded values, so the result is a weighted mean
             pw[u][r / 2] = f2bf2(p0, p1);
@@ -553,6 +581,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) * D <= 256 ? 2 : 1) void k_
 #pragma unroll 1
     for (int j = jm; j < nj; ++j) step(j, std::true_type{});
     l = xor32_sum(l);
+    m *= scl;  // log2 units
 
     // groups add up: group g > 0 leaves its sums in LDS, group 0 takes them in order
     if constexpr (KW > 1) {
@@ -713,13 +742,13 @@ constexpr int kMaxCus = 512;
 Plan plan_of(const PagedView &c, int B, int T, int Hq, int cus) {
   const int rows = T * (Hq / c.Hkv);
   Plan p;
-  p.RW = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  p.KW = 4 / p.RW;
+  p.RW = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || (c.D == 64 && c.dtype == kF8) ? 4 : 8;
+  p.KW = p.RW < 4 ? 4 / p.RW : 1;
   const int TR = 32 * p.RW, IK = p.RW == 1 ? 128 : 64;
   p.nrt = (rows + TR - 1) / TR;
   const long most = ((long)c.max_len + IK - 1) / IK;
   const long items = (long)B * p.nrt * c.Hkv * most;
-  p.W = (int)std::min<long>(items, (long)kWgPerCu * cus);
+  p.W = (int)std::min<long>(items, (long)(p.RW == 8 ? 1 : kWgPerCu) * cus);
   p.join = most > 1 && p.W > 0;
   return p;
 }
@@ -738,7 +767,8 @@ hipError_t launch(const TreeArgs &a, const Plan &p, hipStream_t s) {
 template <typename T, typename S, int D> hipError_t by_rows(const TreeArgs &a, const Plan &p, hipStream_t s) {
   return p.RW == 1 ? launch<T, S, D, 1, 4>(a, p, s)
          : p.RW == 2 ? launch<T, S, D, 2, 2>(a, p, s)
-                     : launch<T, S, D, 4, 1>(a, p, s);
+         : p.RW == 4 || (D == 64 && sizeof(S) == 1) ? launch<T, S, D, 4, 1>(a, p, s)
+                     : launch<T, S, D, D == 64 && sizeof(S) == 1 ? 4 : 8, 1>(a, p, s);
 }
 
 template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Plan &p, hipStream_t s) {
