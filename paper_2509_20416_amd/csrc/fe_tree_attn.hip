@@ -41,15 +41,19 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Keys per tile: 32, or as many as give every lane of RW waves a 16-byte load of an
+// 8-bit row.
+constexpr int tile_keys(int RW, int D) { return RW * 1024 / D > 32 ? RW * 1024 / D : 32; }
+
 // Shape of one variant: RW waves side by side on rows, KW groups of them taking
 // tiles of TK keys in turn.
 template <typename T, int D, int RW_, int KW_> struct Shape {
   static constexpr int RW = RW_, KW = KW_;
-  static constexpr int TK = RW >= 4 ? 64 : 32;   // keys per tile
+  static constexpr int TK = tile_keys(RW, D);
   static constexpr int IK = TK * KW;             // keys per work item
-  static constexpr int TR = 32 * RW;             // rows per tile
+  static constexpr int TR = 32 * RW;        // rows per tile
   static constexpr int NT = 64 * RW * KW;        // threads
-  static constexpr int NBUF = RW == 1 ? 1 : 2;   // LDS buffers per group
+  static constexpr int NBUF = RW == 1 ? 2 : 3;   // LDS buffers per group
   static constexpr int RB = D * (int)sizeof(T);  // bytes per row in LDS
   static constexpr int BUF = 2 * TK * RB;        // K rows, then V rows
   static constexpr int LDS = KW * NBUF * BUF;
@@ -179,8 +183,8 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
     pid = ids(c, table, k0, end);
     pid_next = ids(c, table, min(k0 + 1024, end), end);
   }
-  // Loads tile j of the run (keys k0 ..); rows past end are some row of a page
-  // that belongs to the sequence.
+  // Loads tile j of the run (keys k0 ..); rows past end are some row of a page that
+  // belongs to the sequence.
   __device__ __forceinline__ void load(const PagedView &c, const int32_t *table, int hk, int j, int k0, int end) {
     if (j > 0 && j % WIN == 0) {
       pid = pid_next;
@@ -189,19 +193,19 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
     badp = 0;
     const uint32_t rowb = c.Hkv * D * sizeof(S);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int R0 = i * STEP + rw * SPAN;  // uniform
+    for (int q = 0; q < 2 * NL; ++q) {                  // K's loads, then V's
+      const int i = q % NL, R0 = i * STEP + rw * SPAN;  // uniform
       const int pg = __builtin_amdgcn_readlane(pid, (j % WIN * IK + R0) / 16);
       const bool ok = (unsigned)pg < (unsigned)c.n_pages;
       if (!ok) badp |= 1u << i;
       const long r = ((long)(ok ? pg : 0) << c.shift) + ((k0 + R0) & ((1 << c.shift) - 1));
       const long at = r * rowb + hk * (D * (int)sizeof(S));
-      k[i] = *reinterpret_cast<const u32x4 *>((const char *)c.k + at + loff);
-      v[i] = *reinterpret_cast<const u32x4 *>((const char *)c.v + at + loff);
-      if constexpr (F8) {
-        sk[i] = (c.ks + hk * c.rows() + r)[(uint32_t)lrow];
-        sv[i] = (c.vs + hk * c.rows() + r)[(uint32_t)lrow];
-      }
+      const u32x4 w = *reinterpret_cast<const u32x4 *>((const char *)(q < NL ? c.k : c.v) + at + loff);
+      if (q < NL)
+        k[i] = w;
+      else
+        v[i] = w;
+      if constexpr (F8) (q < NL ? sk : sv)[i] = ((q < NL ? c.ks : c.vs) + hk * c.rows() + r)[(uint32_t)lrow];
     }
   }
   __device__ __forceinline__ static void put(unsigned char *lds, int R, int p, const u32x4 &w, uint32_t s) {
@@ -260,11 +264,29 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
 
 // ---- the kernel -------------------------------------------------------------------
 
+// A value that is the same in every lane, where the compiler can see it (in scalar
+// registers, and branches on it taken by the wave as a whole).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long uniform(long x) {
+  return (long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
 // A value the compiler cannot compute ahead of a seldom taken branch, so that the
 // branch's addresses hold no registers outside it.
 template <typename V> __device__ __forceinline__ V opaque(V x) {
   asm volatile("" : "+v"(x));
   return x;
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+template <typename V> __device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(__attribute__((address_space(3))) const V *)(uintptr_t)at;
+}
+__device__ __forceinline__ u32x2 lds_read_tr(uint32_t at) {
+  return __builtin_bit_cast(
+      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(uintptr_t)at));
 }
 
 // Bytes c .. c + 3 of a mask row of T: one (unaligned) load where T >= 4, moved
@@ -283,16 +305,17 @@ __device__ __forceinline__ uint32_t mask_word(const uint8_t *mp, int c, int T) {
 }
 
 template <typename T, typename S, int D, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
+__global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
   using Sh = Shape<T, D, RW, KW>;
   constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / 32;
   constexpr int VPR = D * (int)sizeof(T) / 16;
-  constexpr int NC = VPR / 2;  // steps of two 16-byte pieces along a key
+  constexpr int NC = VPR / 2;                      // steps of two 16-byte pieces along a key
+  constexpr int NPW = sizeof(T) == 2 ? 8 : 16;     // registers of 32 keys' probabilities
   __shared__ __attribute__((aligned(16))) unsigned char s_mem[Sh::LDS];
   __shared__ float s_ml[KW > 1 ? KW * RW * 64 : 1][2];
   __shared__ long s_scan[NT / 64 + 1];
   __shared__ long s_first[2];
-  __shared__ uint32_t s_odd[2][RW * KW];
+  __shared__ uint32_t s_odd[Sh::NBUF][RW * KW];
   const PagedView &c = a.c;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int grp = wave / RW, rw = wave % RW;
@@ -317,12 +340,12 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
     if (e0 + NT < E) __syncthreads();
   }
   if (blockIdx.x == 0 && tid == 0) work.before()[E] = total;
-  const Ranges rg(total * c.Hkv, W_);
+  const Ranges rg(uniform(total) * c.Hkv, W_);
   if (blockIdx.x >= rg.W) return;
   // neighbouring ranges on one XCD: workgroups go round the 8 of them
   const int xcd = blockIdx.x % 8, wg = (int)(xcd * (rg.W / 8) + min((long)xcd, rg.W % 8)) + blockIdx.x / 8;
   const long x0 = rg.begin(wg), x1 = rg.begin(wg + 1);
-  auto find = [&](int e0) {
+  auto find = [&](int e0) __attribute__((always_inline)) {
     const long lo = before * c.Hkv;
     if (mine > 0 && lo <= x0 && x0 < lo + (long)mine * c.Hkv) {
       s_first[0] = e0 + tid;
@@ -353,9 +376,10 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
   }
   Tile<T, S, D, RW, TK, IK> tile;
   tile.init(c, rw, lane);
-  int e = (int)s_first[0];
-  long at = s_first[1];  // first item of entry e
-  unsigned char *buf = s_mem + grp * Sh::NBUF * Sh::BUF;
+  int e = (int)uniform(s_first[0]);
+  long at = uniform(s_first[1]);  // first item of entry e
+  unsigned char *bufs = s_mem + grp * Sh::NBUF * Sh::BUF;
+  const uint32_t bufs_at = lds_address(bufs);
 
   for (long x = x0; x < x1;) {
     const int it = items_of(a, e, nrt, TR, IK);
@@ -369,219 +393,227 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
     x += ni;
     const Span sp = span_of(a, b);
     const int end = keys_end(a, sp, rt, TR);
-    // this lane's row: node, head
-    const int row = rt * TR + 32 * rw + n32, rowc = min(row, sp.live - 1);
-    const int node = rowc / G, head = hk * G + rowc % G;
     const int vis_all = sp.bad ? 0 : sp.P + (a.mask ? 0 : rt * TR / G + 1);  // keys every row sees
     const int32_t *table = c.pages + (size_t)b * c.max_pages;
-
-    // q, 16 bytes of two neighbouring pieces per step: the right operand
+    const int kbeg = i0 * IK + grp * TK;
+    // the group's tiles: keys kbeg + j * IK, j < nj (as many rounds for every group)
+    const int nj = end > i0 * IK ? min(ni, (end - i0 * IK + IK - 1) / IK) : 0;
+    auto has = [&](int j) __attribute__((always_inline)) { return j < nj && kbeg + j * IK < end; };
+    if (has(0)) {
+      tile.pages(c, table, kbeg, end);
+      tile.load(c, table, hk, 0, kbeg, end);
+    }
+    // this lane's row: node, head, and q, 16 bytes of two neighbouring pieces per
+    // step: the right operand
+    const int row = rt * TR + 32 * rw + n32, rowc = min(row, sp.live - 1);
+    const int node = rowc / G, head = hk * G + rowc % G;
     u32x4 qf[NC];
     {
       const T *qp = (const T *)a.q + ((long)b * a.T + node) * a.qs + (long)head * D;
 #pragma unroll
       for (int cc = 0; cc < NC; ++cc) qf[cc] = *reinterpret_cast<const u32x4 *>((const char *)qp + 16 * (2 * cc + h));
     }
+    const bool wlive = rt * TR + 32 * rw < sp.live;  // some row of this wave is there
+    const float scl = a.scale * kLog2e;
+    float m = -INFINITY, l = 0.f;  // running maximum (log2 units) and sum
     f32x16 o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x16(0.f);
-    // the running maximum in the scores' own units, and 16 copies of its negative
-    // that the first product starts from: scores come out relative to it
-    float m = -INFINITY, l = 0.f;
-    f32x16 base = f32x16(0.f);
-    const float scl = a.scale * kLog2e, inv_scl = 1.f / scl;
-    const bool wlive = rt * TR + 32 * rw < sp.live;  // some row of this wave is there
+    uint32_t pw[NPW];      // probabilities as the second product takes them
+    uint32_t seen = ~0u;   // bit r: register r's key is seen
 
-    const int kbeg = i0 * IK + grp * TK;
-    // the group's tiles: keys kbeg + j * IK, j < nj (as many rounds for every group)
-    const int nj = end > i0 * IK ? min(ni, (end - i0 * IK + IK - 1) / IK) : 0;
-    auto has = [&](int j) { return j < nj && kbeg + j * IK < end; };
-    if (has(0)) {
-      tile.pages(c, table, kbeg, end);
-      tile.load(c, table, hk, 0, kbeg, end);
-    }
-    // tile j; kMasked: some row may not see all of it (the last tiles)
-    auto step = [&](int j, auto kMasked) {
-      constexpr bool masked = decltype(kMasked)::value;
-      const int k0 = kbeg + j * IK;
-      const bool live = !masked || has(j);
-      unsigned char *kb = buf + (Sh::NBUF == 2 ? (j & 1) * Sh::BUF : 0);
-      uint32_t odd = 0;
-      if (live) {
-        odd = __builtin_amdgcn_ballot_w64(tile.template store<masked>(kb, end - k0)) != 0;
-        if (masked && RW > 1 && lane == 0) s_odd[j & 1][wave] = odd;
+    // Tile j into its buffer.  Behind barrier j + 1 every wave may read tile j + 1;
+    // a wave may still read values of tile j - 1 until barrier j + 1: three buffers
+    // (two where a wave shares them with no other).
+    uint32_t odd_own = 0;  // bit: this wave's part of the tile in that buffer holds a value that is not finite
+    auto put = [&](int j) __attribute__((always_inline)) {
+      const int k0 = kbeg + j * IK, at_buf = j % Sh::NBUF;
+      unsigned char *kb = bufs + at_buf * Sh::BUF;
+      if (k0 + TK > vis_all) {
+        const bool odd = __builtin_amdgcn_ballot_w64(tile.template store<true>(kb, end - k0)) != 0;
+        if (RW > 1 && lane == 0) s_odd[at_buf][wave] = odd;
+        odd_own = (odd_own & ~(1u << at_buf)) | (uint32_t)odd << at_buf;
+      } else {
+        tile.template store<false>(kb, TK);
       }
-      if (has(j + 1)) tile.load(c, table, hk, j + 1, k0 + IK, end);
-      if constexpr (RW > 1) __syncthreads();
-      if (!live || !wlive) return;
-      const unsigned char *vb = kb + TK * Sh::RB;
-
-      // S^T = K Q^T: keys 32 sub + n32 as rows
-      f32x16 s[NS];
+    };
+    // S^T = K Q^T, then probabilities and their sum.
+    auto scores = [&](int j, int u, auto kMasked) __attribute__((always_inline)) {
+      const int k0 = kbeg + j * IK + 32 * u;
+      // 16-byte piece 2 cc + h of row n32: ^ 32 cc
+      const uint32_t ka = opaque(bufs_at + (j % Sh::NBUF) * Sh::BUF + 32 * u * Sh::RB + 16 * piece_at<VPR>(n32, h));
+      f32x16 s = f32x16(0.f);
 #pragma unroll
-      for (int u = 0; u < NS; ++u) s[u] = base;
+      for (int cc = 0; cc < NC; ++cc) {
+        const u32x4 kf = lds_read<u32x4>(ka ^ (32 * cc));
+        if constexpr (sizeof(T) == 2) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[cc]),
+                                                      s, 0, 0, 0);
+        } else {
+          const f32x4 kv = __builtin_bit_cast(f32x4, kf), qv = __builtin_bit_cast(f32x4, qf[cc]);
 #pragma unroll
-      for (int cc = 0; cc < NC; ++cc)
-#pragma unroll
-        for (int u = 0; u < NS; ++u) {
-          const u32x4 kf = reinterpret_cast<const u32x4 *>(kb)[piece_at<VPR>(32 * u + n32, 2 * cc + h)];
-          if constexpr (sizeof(T) == 2) {
-            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                           __builtin_bit_cast(bf16x8, qf[cc]), s[u], 0, 0, 0);
-          } else {
-            const f32x4 ka = __builtin_bit_cast(f32x4, kf), qa = __builtin_bit_cast(f32x4, qf[cc]);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(ka[w], qa[w], s[u], 0, 0, 0);
-          }
+          for (int w = 0; w < 4; ++w) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[w], qv[w], s, 0, 0, 0);
         }
-      // register r of sub-tile u: key 32 u + 8 (r / 4) + 4 h + r % 4
-      [[maybe_unused]] uint32_t seen[NS];  // bit r: register r's key is seen
-      if constexpr (masked) {
+      }
+      // log2 units from the maximum on; register r: key k0 + 8 (r / 4) + 4 h + r % 4
+      const float mr = m == -INFINITY ? 0.f : m;
+      s = s * scl - mr;
+      if constexpr (decltype(kMasked)::value) {
         const uint8_t *mp = opaque(a.mask ? a.mask + ((size_t)b * a.T + node) * a.T : nullptr);
         const int c0 = opaque(k0 - sp.P + 4 * h);
+        uint32_t sn = 0;
 #pragma unroll
-        for (int u = 0; u < NS; ++u) {
-          seen[u] = 0;
+        for (int i = 0; i < 4; ++i) {  // four neighbouring keys
+          const int cn = c0 + 8 * i;
+          const uint32_t own = mp ? mask_word(mp, cn, a.T) : 0u;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {  // four neighbouring keys
-            const int cn = c0 + 32 * u + 8 * i;
-            const uint32_t own = mp ? mask_word(mp, cn, a.T) : 0u;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const uint32_t in_mask = mp ? (own >> 8 * v & 255) != 0 : cn + v <= node;
-              const uint32_t inside = cn + v < sp.n;
-              seen[u] |= ((uint32_t)(cn + v < 0) | (inside & in_mask)) << (4 * i + v);
-            }
+          for (int v = 0; v < 4; ++v) {
+            const uint32_t in_mask = mp ? (own >> 8 * v & 255) != 0 : cn + v <= node;
+            const uint32_t inside = cn + v < sp.n;
+            sn |= ((uint32_t)(cn + v < 0) | (inside & in_mask)) << (4 * i + v);
           }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][r] = (seen[u] >> r & 1) ? s[u][r] : -INFINITY;
         }
+        seen = sn;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = (sn >> r & 1) ? s[r] : -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < NS; ++u) {
-        s[u] *= scl;
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[u][r]), s[u][r + 1]);
-      }
+      for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
       mx = xor32_max(mx);
       // the maximum is raised only when a score passes it by 2^8: probabilities
       // stay below that, and the accumulators are seldom rescaled
       const bool up = mx > (m == -INFINITY ? -INFINITY : kLazyMax);
       if (__builtin_amdgcn_ballot_w64(up)) {
         const float by = up ? mx : 0.f, alpha = __builtin_amdgcn_exp2f(-by);
-        if (up) m = (m == -INFINITY ? 0.f : m) + by * inv_scl;
-        base = f32x16(m == -INFINITY ? 0.f : -m);
+        if (up) m = mr + by;
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
-#pragma unroll
-        for (int u = 0; u < NS; ++u) s[u] -= by;
+        s -= by;
       }
-      uint32_t pw[NS][sizeof(T) == 2 ? 8 : 16];   // probabilities, as the product takes them
 #pragma unroll
-      for (int u = 0; u < NS; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(s[u][r]);
-          const float p1 = __builtin_amdgcn_exp2f(s[u][r + 1]);
-          if constexpr (sizeof(T) == 2) {
-            // the sum takes the rounded values, so the result is a weighted mean
-            pw[u][r / 2] = f2bf2(p0, p1);
-            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[u][r / 2]),
-                                                __builtin_bit_cast(bf16x2_t, 0x3f803f80u), l, false);
-          } else {
-            pw[u][r] = __float_as_uint(p0);
-            pw[u][r + 1] = __float_as_uint(p1);
-            l += p0 + p1;
-          }
+      for (int r = 0; r < 16; r += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]);
+        if constexpr (sizeof(T) == 2) {
+          // the sum takes the rounded values, so the result is a weighted mean
+          pw[r / 2] = f2bf2(p0, p1);
+          l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[r / 2]),
+                                              __builtin_bit_cast(bf16x2_t, 0x3f803f80u), l, false);
+        } else {
+          pw[r] = __float_as_uint(p0);
+          pw[r + 1] = __float_as_uint(p1);
+          l += p0 + p1;
         }
-      if constexpr (masked) {
+      }
+    };
+    // O^T += V^T P^T.
+    auto values = [&](int j, int u, auto kMasked) __attribute__((always_inline)) {
+      const uint32_t vb = bufs_at + (j % Sh::NBUF) * Sh::BUF + (TK + 32 * u) * Sh::RB;
+      bool odd = false;
+      if constexpr (decltype(kMasked)::value) {
+        odd = odd_own >> (j % Sh::NBUF) & 1;
         if constexpr (RW > 1) {
 #pragma unroll
-          for (int w = 0; w < RW; ++w) odd |= s_odd[j & 1][grp * RW + w];
-        }
-        if (odd) {
-          // a value row that some row does not see may hold an infinity or NaN:
-          // key by key, every row over the keys it sees
-#pragma unroll 1
-          for (int key = 0; key < TK; ++key) {
-            const int hh = opaque(h);
-            const int u0 = key >> 5, r0 = (key >> 3 & 3) * 4 + (key & 3), from = n32 + 32 * (key >> 2 & 1);
-            uint32_t w = 0, sn = 0;
-#pragma unroll
-            for (int u = 0; u < NS; ++u)
-              if (u == u0) {
-                sn = seen[u];
-#pragma unroll
-                for (int r = 0; r < (sizeof(T) == 2 ? 8 : 16); ++r)
-                  if (r == (sizeof(T) == 2 ? r0 / 2 : r0)) w = pw[u][r];
-              }
-            w = __shfl(w, from, 64);
-            sn = __shfl(sn, from, 64);
-            const float p = sizeof(T) == 4 ? __uint_as_float(w)
-                                           : __uint_as_float((r0 & 1) ? w & 0xffff0000u : w << 16);
-            const bool vis = sn >> r0 & 1;
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-              for (int g8 = 0; g8 < 4; ++g8) {
-                const int d0 = 32 * dt + 8 * g8 + 4 * hh, by = d0 * (int)sizeof(T);
-                const T *vp = reinterpret_cast<const T *>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
-#pragma unroll
-                for (int w4 = 0; w4 < 4; ++w4)
-                  if (vis) o[dt][4 * g8 + w4] += p * Elt<T>::to_f(vp[w4]);
-              }
-          }
-          return;
+          for (int w = 0; w < RW; ++w) odd |= s_odd[j % Sh::NBUF][grp * RW + w] != 0;
         }
       }
-      // O^T += V^T P^T over the tile's keys
+      if (odd) {
+        // a value row that some row does not see may hold an infinity or NaN: key by
+        // key, every row over the keys it sees
+#pragma unroll 1
+        for (int key = 0; key < 32; ++key) {
+          const int hh = opaque(h), r0 = (key >> 3) * 4 + (key & 3), from = n32 + 32 * (key >> 2 & 1);
+          uint32_t w = 0;
 #pragma unroll
-      for (int u = 0; u < NS; ++u) {
-        if constexpr (sizeof(T) == 2) {
+          for (int r = 0; r < NPW; ++r)
+            if (r == (sizeof(T) == 2 ? r0 / 2 : r0)) w = pw[r];
+          w = __shfl(w, from, 64);
+          const uint32_t sn = __shfl(seen, from, 64);
+          const float p =
+              sizeof(T) == 4 ? __uint_as_float(w) : __uint_as_float((r0 & 1) ? w & 0xffff0000u : w << 16);
+          const bool vis = sn >> r0 & 1;
 #pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const u32x4 pf = {pw[u][2 * i], pw[u][2 * i + 1], pw[u][2 * i + 2], pw[u][2 * i + 3]};
+          for (int dt = 0; dt < NDT; ++dt) {
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) {
-              // keys 8 i + 4 h + 0 .. 3 and the same 8 further, dim 32 dt + n32: the
-              // transposing read (lane 4 e + q of 16 names key e, dims 4 q .. + 3)
-              const int R = 32 * u + 8 * i + 4 * h + (lane >> 2 & 3);
-              const int p = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-              auto tr = [&](int key) {
-                return __builtin_bit_cast(
-                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(
-                               vb + 16 * piece_at<VPR>(key, p) + 8 * (lane & 1))));
-              };
-              const u32x2 v0 = tr(R), v1 = tr(R + 8);
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  __builtin_bit_cast(bf16x8, (u32x4{v0.x, v0.y, v1.x, v1.y})), __builtin_bit_cast(bf16x8, pf),
-                  o[dt], 0, 0, 0);
+            for (int g8 = 0; g8 < 4; ++g8) {
+              const int by = (32 * dt + 8 * g8 + 4 * hh) * (int)sizeof(T);
+              const uint32_t va = vb + 16 * piece_at<VPR>(key, by / 16) + by % 16;
+              f32x4 vw;
+              if constexpr (sizeof(T) == 2) {
+                const u32x2 w2 = lds_read<u32x2>(va);
+                vw = f32x4{__uint_as_float(w2.x << 16), __uint_as_float(w2.x & 0xffff0000u),
+                           __uint_as_float(w2.y << 16), __uint_as_float(w2.y & 0xffff0000u)};
+              } else {
+                vw = lds_read<f32x4>(va);
+              }
+#pragma unroll
+              for (int w4 = 0; w4 < 4; ++w4)
+                o[dt][4 * g8 + w4] = vis ? o[dt][4 * g8 + w4] + p * vw[w4] : o[dt][4 * g8 + w4];
             }
+            __builtin_amdgcn_sched_barrier(0);  // no loads ahead: registers are short here
           }
-        } else {
+        }
+        return;
+      }
+      if constexpr (sizeof(T) == 2) {
+        // keys 8 i + 4 h + 0 .. 3 (i even) and the same 8 further, dim 32 dt + n32: the
+        // transposing read (lane 4 e + q of 16 names key e, dims 4 q .. + 3); the dims
+        // of step dt lie ^ 64 dt
+        const int R = 4 * h + (lane >> 2 & 3), pc = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        const uint32_t va0 = opaque(vb + 16 * piece_at<VPR>(R, pc) + 8 * (lane & 1));
+        const uint32_t va1 = opaque(vb + 16 * piece_at<VPR>(R + 8, pc) + 8 * (lane & 1));
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = 32 * u + 8 * (r / 4) + 4 * h + r % 4;
+        for (int i = 0; i < 4; i += 2) {
+          const u32x4 pf = {pw[2 * i], pw[2 * i + 1], pw[2 * i + 2], pw[2 * i + 3]};
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) {
-              const int by = 4 * (32 * dt + n32);
-              const float vf = *reinterpret_cast<const float *>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, __uint_as_float(pw[u][r]), o[dt], 0, 0, 0);
-            }
+          for (int dt = 0; dt < NDT; ++dt) {
+            const u32x2 v0 = lds_read_tr((va0 ^ (64 * dt)) + 8 * i * Sh::RB);
+            const u32x2 v1 = lds_read_tr((va1 ^ (64 * dt)) + 8 * i * Sh::RB);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, (u32x4{v0.x, v0.y, v1.x, v1.y})),
+                                                            __builtin_bit_cast(bf16x8, pf), o[dt], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = 8 * (r / 4) + 4 * h + r % 4;
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const int by = 4 * (32 * dt + n32);
+            const float vf = lds_read<float>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, __uint_as_float(pw[r]), o[dt], 0, 0, 0);
           }
         }
       }
     };
-    const int room = vis_all - TK - kbeg;  // the first tile that is masked starts behind it
+    if (has(0)) put(0);
+    if (has(1)) tile.load(c, table, hk, 1, kbeg + IK, end);
+    auto step = [&](int j, auto kMasked) __attribute__((always_inline)) {
+      if constexpr (RW > 1) __syncthreads();
+      if (decltype(kMasked)::value && !has(j)) return;
+      if (wlive) {
+        scores(j, 0, kMasked);
+        values(j, 0, kMasked);
+      }
+      if (has(j + 1)) put(j + 1);
+      if (has(j + 2)) tile.load(c, table, hk, j + 2, kbeg + (j + 2) * IK, end);
+      if (wlive) {
+#pragma unroll 1
+        for (int u = 1; u < NS; ++u) {
+          scores(j, u, kMasked);
+          values(j, u, kMasked);
+        }
+      }
+    };
+    // whole tiles that every row sees, then the others
+    const int room = vis_all - TK - kbeg;
     const int jm = room < 0 ? 0 : min(nj, room / IK + 1);
 #pragma unroll 1
     for (int j = 0; j < jm; ++j) step(j, std::false_type{});
 #pragma unroll 1
     for (int j = jm; j < nj; ++j) step(j, std::true_type{});
     l = xor32_sum(l);
-    m *= scl;  // log2 units
 
     // groups add up: group g > 0 leaves its sums in LDS, group 0 takes them in order
     if constexpr (KW > 1) {
@@ -589,33 +621,35 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       static_assert((KW - 1) * RW * (D / 8) * 64 * 16 <= Sh::LDS, "sums fit the tiles' buffers");
       __syncthreads();
       if (grp > 0) {
+        const int at_w = (grp - 1) * RW + rw;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
           for (int g8 = 0; g8 < 4; ++g8)
-            so[(((grp - 1) * RW + rw) * (D / 8) + 4 * dt + g8) * 64 + lane] =
+            so[(at_w * (D / 8) + 4 * dt + g8) * 64 + lane] =
                 f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
-        s_ml[wave * 64 + lane][0] = m;
-        s_ml[wave * 64 + lane][1] = l;
+        s_ml[at_w * 64 + lane][0] = m;
+        s_ml[at_w * 64 + lane][1] = l;
       }
       __syncthreads();
       if (grp == 0) {
         float mm = m;
 #pragma unroll
-        for (int g = 1; g < KW; ++g) mm = fmaxf(mm, s_ml[(g * RW + rw) * 64 + lane][0]);
+        for (int g = 1; g < KW; ++g) mm = fmaxf(mm, s_ml[((g - 1) * RW + rw) * 64 + lane][0]);
         const float sc0 = sexp2(m, mm);
         l *= sc0;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o[dt] *= sc0;
-#pragma unroll
+#pragma unroll 1
         for (int g = 1; g < KW; ++g) {
-          const float scg = sexp2(s_ml[(g * RW + rw) * 64 + lane][0], mm);
-          l += s_ml[(g * RW + rw) * 64 + lane][1] * scg;
+          const int at_w = (g - 1) * RW + rw;
+          const float scg = sexp2(s_ml[at_w * 64 + lane][0], mm);
+          l += s_ml[at_w * 64 + lane][1] * scg;
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
             for (int g8 = 0; g8 < 4; ++g8) {
-              const f32x4 w = so[(((g - 1) * RW + rw) * (D / 8) + 4 * dt + g8) * 64 + lane];
+              const f32x4 w = so[(at_w * (D / 8) + 4 * dt + g8) * 64 + lane];
 #pragma unroll
               for (int w4 = 0; w4 < 4; ++w4) o[dt][4 * g8 + w4] += w[w4] * scg;
             }
@@ -624,8 +658,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       }
     }
     if (grp == 0 && row < sp.live) {
-      const bool head_cut = i0 > 0, whole = ni == it;
-      if (whole) {
+      if (ni == it) {  // the whole segment
         const float inv = sp.bad ? __int_as_float(0x7fc00000) : l == 0.f ? 0.f : 1.f / l;
         T *op = (T *)a.out + (((long)b * a.T + node) * a.Hq + head) * D + 4 * h;
 #pragma unroll
@@ -639,7 +672,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
               *reinterpret_cast<f32x4 *>(op + 32 * dt + 8 * g8) = w;
           }
       } else {
-        const long slot = 2L * wg + (head_cut ? 0 : 1);
+        const long slot = 2L * wg + (i0 > 0 ? 0 : 1);
         const int rr = 32 * rw + n32;
         float *po = work.o(slot) + (long)rr * D + 4 * h;
 #pragma unroll
@@ -728,47 +761,56 @@ int compute_units() {
   return n;
 }
 
-// The launch of a call: rows per tile, keys per work item, row tiles per sequence,
-// ranges, and whether a segment may be cut at all.
+// The launch of a call: the variant, row tiles per sequence, ranges, and whether a
+// segment may be cut at all.
 struct Plan {
-  int RW, KW, nrt, W;
+  int variant, nrt, W;
   bool join;
 };
-
-// Workgroups: two per compute unit, no more than there can be work items.
-constexpr int kWgPerCu = 2;
 constexpr int kMaxCus = 512;
 
-Plan plan_of(const PagedView &c, int B, int T, int Hq, int cus) {
+// Variants by rows per (sequence, KV head): RW, KW.  The last two are fp32's,
+// whose keys take twice the LDS and whose operands twice the registers.
+constexpr int kShapes[6][2] = {{1, 4}, {2, 2}, {4, 2}, {8, 1}, {1, 2}, {4, 1}};
+
+int variant_of(int rows, int dt) {
+  if (dt == kF32) return rows <= 32 ? 4 : 5;
+  return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3;
+}
+
+Plan plan_of(const PagedView &c, int B, int T, int Hq, int dt, int cus) {
   const int rows = T * (Hq / c.Hkv);
   Plan p;
-  p.RW = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || (c.D == 64 && c.dtype == kF8) ? 4 : 8;
-  p.KW = p.RW < 4 ? 4 / p.RW : 1;
-  const int TR = 32 * p.RW, IK = p.RW == 1 ? 128 : 64;
+  p.variant = variant_of(rows, dt);
+  const int *sh = kShapes[p.variant];
+  const int TR = 32 * sh[0], IK = sh[1] * tile_keys(sh[0], c.D);
   p.nrt = (rows + TR - 1) / TR;
   const long most = ((long)c.max_len + IK - 1) / IK;
   const long items = (long)B * p.nrt * c.Hkv * most;
-  p.W = (int)std::min<long>(items, (long)(p.RW == 8 ? 1 : kWgPerCu) * cus);
+  p.W = (int)std::min<long>(items, cus);
   p.join = most > 1 && p.W > 0;
   return p;
 }
 
-template <typename T, typename S, int D, int RW, int KW>
-hipError_t launch(const TreeArgs &a, const Plan &p, hipStream_t s) {
-  k_tree_attn<T, S, D, RW, KW><<<p.W, 64 * RW * KW, 0, s>>>(a, p.nrt, p.W);
+template <typename T, typename S, int D, int V> hipError_t launch(const TreeArgs &a, const Plan &p, hipStream_t s) {
+  using Sh = Shape<T, D, kShapes[V][0], kShapes[V][1]>;
+  k_tree_attn<T, S, D, Sh::RW, Sh::KW><<<p.W, Sh::NT, 0, s>>>(a, p.nrt, p.W);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.join) return e;
-  constexpr int TR = 32 * RW;
-  const int rows = std::min<long>(TR, (long)a.T * (a.Hq / a.c.Hkv));
-  k_tree_join<T, D><<<dim3(a.B * p.nrt * a.c.Hkv, (rows * D + 1023) / 1024), 256, 0, s>>>(a, p.nrt, p.W, TR);
+  const int rows = std::min<long>(Sh::TR, (long)a.T * (a.Hq / a.c.Hkv));
+  k_tree_join<T, D><<<dim3(a.B * p.nrt * a.c.Hkv, (rows * D + 1023) / 1024), 256, 0, s>>>(a, p.nrt, p.W, Sh::TR);
   return hipGetLastError();
 }
 
 template <typename T, typename S, int D> hipError_t by_rows(const TreeArgs &a, const Plan &p, hipStream_t s) {
-  return p.RW == 1 ? launch<T, S, D, 1, 4>(a, p, s)
-         : p.RW == 2 ? launch<T, S, D, 2, 2>(a, p, s)
-         : p.RW == 4 || (D == 64 && sizeof(S) == 1) ? launch<T, S, D, 4, 1>(a, p, s)
-                     : launch<T, S, D, D == 64 && sizeof(S) == 1 ? 4 : 8, 1>(a, p, s);
+  if constexpr (sizeof(T) == 4) {
+    return p.variant == 4 ? launch<T, S, D, 4>(a, p, s) : launch<T, S, D, 5>(a, p, s);
+  } else {
+    return p.variant == 0   ? launch<T, S, D, 0>(a, p, s)
+           : p.variant == 1 ? launch<T, S, D, 1>(a, p, s)
+           : p.variant == 2 ? launch<T, S, D, 2>(a, p, s)
+                            : launch<T, S, D, 3>(a, p, s);
+  }
 }
 
 template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Plan &p, hipStream_t s) {
@@ -777,14 +819,14 @@ template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Pla
 
 }  // namespace
 
-size_t tree_attention_ws(const PagedView &c, int B, int T, int Hq, int) {
-  const Plan p = plan_of(c, B, T, Hq, kMaxCus);
-  const size_t rows = 2 * (size_t)p.W * 32 * p.RW;
+size_t tree_attention_ws(const PagedView &c, int B, int T, int Hq, int dt) {
+  const Plan p = plan_of(c, B, T, Hq, dt, kMaxCus);
+  const size_t rows = 2 * (size_t)p.W * 32 * kShapes[p.variant][0];
   return (rows * (c.D + 2) * 4 + ((size_t)B * p.nrt + 1) * 8 + 255) & ~(size_t)255;
 }
 
 hipError_t tree_attention(const TreeArgs &a, int dt, hipStream_t s) {
-  const Plan p = plan_of(a.c, a.B, a.T, a.Hq, std::min(compute_units(), kMaxCus));
+  const Plan p = plan_of(a.c, a.B, a.T, a.Hq, dt, std::min(compute_units(), kMaxCus));
   if (dt == kF32) return a.c.dtype == kF8 ? by_dim<float, uint8_t>(a, p, s) : by_dim<float, float>(a, p, s);
   return a.c.dtype == kF8 ? by_dim<uint16_t, uint8_t>(a, p, s) : by_dim<uint16_t, uint16_t>(a, p, s);
 }
