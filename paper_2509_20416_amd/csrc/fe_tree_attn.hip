@@ -83,7 +83,13 @@ __device__ __forceinline__ int keys_end(const TreeArgs &a, const Span &s, int rt
   if (a.mask) return s.P + s.n;
   return s.P + (min((rt + 1) * TR, s.live) - 1) / (a.Hq / a.c.Hkv) + 1;
 }
-// Work items of a segment (none where the tile has no row).
+// Starting and ending a segment costs about as much as kSegItems of its work items
+// (its lengths, pages, queries and first keys are fetched one after the other, and
+// its sums written), so where every workgroup gets several items a segment counts
+// that many more.
+constexpr int kSegItems = 3;
+
+// Work items of a segment: steps over its keys (none where the tile has no row).
 __device__ __forceinline__ int items_of(const TreeArgs &a, int e, int nrt, int TR, int IK) {
   const Span s = span_of(a, e / nrt);
   const int rt = e % nrt;
@@ -313,7 +319,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn
   constexpr int NPW = sizeof(T) == 2 ? 8 : 16;     // registers of 32 keys' probabilities
   __shared__ __attribute__((aligned(16))) unsigned char s_mem[Sh::LDS];
   __shared__ float s_ml[KW > 1 ? KW * RW * 64 : 1][2];
-  __shared__ long s_scan[NT / 64 + 1];
+  __shared__ long s_scan[NT / 64];
+  __shared__ int s_segs[NT / 64];
   __shared__ long s_first[2];
   __shared__ uint32_t s_odd[Sh::NBUF][RW * KW];
   const PagedView &c = a.c;
@@ -323,57 +330,71 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn
   const int G = a.Hq / c.Hkv, E = a.B * nrt;
   // the items of every segment, this range of them, and the segment it starts in
   Work<D> work{a.ws, 2L * W_, TR};
-  long total = 0, before = 0;
+  long total = 0, before = 0;  // items of all, and of those before this thread's
+  int segs = 0, segs_before = 0;
   uint32_t mine = 0;
-  for (int e0 = 0; e0 < E; e0 += NT) {
+  // The counts of NT entries, added to the running sums.
+  auto count = [&](int e0, long &sum, int &nseg) __attribute__((always_inline)) {
     mine = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
     const uint32_t inc = wave_incl_scan(mine);
-    if (lane == 63) s_scan[wave] = inc;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(mine > 0);
+    if (lane == 63) {
+      s_scan[wave] = inc;
+      s_segs[wave] = __popcll(some);
+    }
     __syncthreads();
-    before = total + inc - mine;
+    before = sum + inc - mine;
+    segs_before = nseg + __popcll(some & ((1ull << lane) - 1));
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-      if (w < wave) before += s_scan[w];
-      total += s_scan[w];
+      if (w < wave) {
+        before += s_scan[w];
+        segs_before += s_segs[w];
+      }
+      sum += s_scan[w];
+      nseg += s_segs[w];
     }
-    if (blockIdx.x == 0 && e0 + tid < E) work.before()[e0 + tid] = before;
-    if (e0 + NT < E) __syncthreads();
+  };
+  for (int e0 = 0; e0 < E; e0 += NT) {
+    if (e0 > 0) __syncthreads();
+    count(e0, total, segs);
   }
-  if (blockIdx.x == 0 && tid == 0) work.before()[E] = total;
-  const Ranges rg(uniform(total) * c.Hkv, W_);
+  total = uniform(total);
+  segs = uniform(segs);
+  const int extra = total * c.Hkv > 2L * W_ ? kSegItems : 0;
+  const Ranges rg((total + (long)extra * segs) * c.Hkv, W_);
+  if (rg.total == 0) {
+    if (blockIdx.x == 0)
+      for (int e0 = tid; e0 <= E; e0 += NT) work.before()[e0] = 0;
+    return;
+  }
   if (blockIdx.x >= rg.W) return;
   // neighbouring ranges on one XCD: workgroups go round the 8 of them
   const int xcd = blockIdx.x % 8, wg = (int)(xcd * (rg.W / 8) + min((long)xcd, rg.W % 8)) + blockIdx.x / 8;
   const long x0 = rg.begin(wg), x1 = rg.begin(wg + 1);
   auto find = [&](int e0) __attribute__((always_inline)) {
+    before += (long)extra * segs_before;
+    if (blockIdx.x == 0 && e0 + tid < E) work.before()[e0 + tid] = before;
     const long lo = before * c.Hkv;
-    if (mine > 0 && lo <= x0 && x0 < lo + (long)mine * c.Hkv) {
+    if (mine > 0 && lo <= x0 && x0 < lo + (long)(mine + extra) * c.Hkv) {
       s_first[0] = e0 + tid;
       s_first[1] = lo;
     }
   };
   if (E <= NT) {
     find(0);
-    __syncthreads();
   } else {  // a second walk: the first kept only its last stretch
-    long run = 0;
+    long sum = 0;
+    int nseg = 0;
     for (int e0 = 0; e0 < E; e0 += NT) {
       __syncthreads();
-      mine = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
-      const uint32_t inc = wave_incl_scan(mine);
-      if (lane == 63) s_scan[wave] = inc;
-      __syncthreads();
-      before = run + inc - mine;
-#pragma unroll
-      for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) before += s_scan[w];
-        run += s_scan[w];
-      }
+      count(e0, sum, nseg);
       find(e0);
-      if (run * c.Hkv > x0) break;
+      if (blockIdx.x > 0 && (uniform(sum) + (long)extra * uniform(nseg)) * c.Hkv > x0) break;
     }
-    __syncthreads();
   }
+  if (blockIdx.x == 0 && tid == 0) work.before()[E] = rg.total / c.Hkv;
+  __syncthreads();
   Tile<T, S, D, RW, TK, IK> tile;
   tile.init(c, rw, lane);
   int e = (int)uniform(s_first[0]);
@@ -382,7 +403,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn
   const uint32_t bufs_at = lds_address(bufs);
 
   for (long x = x0; x < x1;) {
-    const int it = items_of(a, e, nrt, TR, IK);
+    const int steps = items_of(a, e, nrt, TR, IK), it = steps > 0 ? steps + extra : 0;
     if (it == 0 || x >= at + (long)it * c.Hkv) {
       at += (long)it * c.Hkv;
       ++e;
@@ -397,7 +418,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn
     const int32_t *table = c.pages + (size_t)b * c.max_pages;
     const int kbeg = i0 * IK + grp * TK;
     // the group's tiles: keys kbeg + j * IK, j < nj (as many rounds for every group)
-    const int nj = end > i0 * IK ? min(ni, (end - i0 * IK + IK - 1) / IK) : 0;
+    const int nj = i0 < steps && end > 0 ? min(ni, steps - i0) : 0;
     auto has = [&](int j) __attribute__((always_inline)) { return j < nj && kbeg + j * IK < end; };
     if (has(0)) {
       tile.pages(c, table, kbeg, end);
@@ -731,7 +752,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int nrt, int W_, 
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const float su = __shfl(sc, min(i + u, GL - 1), GL);
-        if (i + u < n) o += part[u] * su;
+        if (i + u < n && su > 0.f) o += part[u] * su;
       }
     }
   }
