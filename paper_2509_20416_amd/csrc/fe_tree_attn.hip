@@ -53,7 +53,7 @@ template <typename T, int D, int RW_, int KW_> struct Shape {
   static constexpr int IK = TK * KW;             // keys per work item
   static constexpr int TR = 32 * RW;        // rows per tile
   static constexpr int NT = 64 * RW * KW;        // threads
-  static constexpr int NBUF = RW == 1 ? 2 : 3;   // LDS buffers per group
+  static constexpr int NBUF = RW == 1 ? 1 : 2;   // LDS buffers per group
   static constexpr int RB = D * (int)sizeof(T);  // bytes per row in LDS
   static constexpr int BUF = 2 * TK * RB;        // K rows, then V rows
   static constexpr int LDS = KW * NBUF * BUF;
@@ -311,7 +311,7 @@ __device__ __forceinline__ uint32_t mask_word(const uint8_t *mp, int c, int T) {
 }
 
 template <typename T, typename S, int D, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
   using Sh = Shape<T, D, RW, KW>;
   constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / 32;
   constexpr int VPR = D * (int)sizeof(T) / 16;
@@ -443,9 +443,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW > 4 ? 2 : 1) void k_tree_attn
     uint32_t pw[NPW];      // probabilities as the second product takes them
     uint32_t seen = ~0u;   // bit r: register r's key is seen
 
-    // Tile j into its buffer.  Behind barrier j + 1 every wave may read tile j + 1;
-    // a wave may still read values of tile j - 1 until barrier j + 1: three buffers
-    // (two where a wave shares them with no other).
+    // Tile j + 1 into its buffer, between barriers j and j + 1: tile j - 1's readers
+    // are past barrier j.  (A wave that shares its tiles with no other needs one
+    // buffer: its reads of tile j come before.)
     uint32_t odd_own = 0;  // bit: this wave's part of the tile in that buffer holds a value that is not finite
     auto put = [&](int j) __attribute__((always_inline)) {
       const int k0 = kbeg + j * IK, at_buf = j % Sh::NBUF;
@@ -790,13 +790,13 @@ struct Plan {
 };
 constexpr int kMaxCus = 512;
 
-// Variants by rows per (sequence, KV head): RW, KW.  The last two are fp32's,
-// whose keys take twice the LDS and whose operands twice the registers.
-constexpr int kShapes[6][2] = {{1, 4}, {2, 2}, {4, 2}, {8, 1}, {1, 2}, {4, 1}};
+// Variants by rows per (sequence, KV head): RW, KW, workgroups per compute unit.
+// The last is fp32's, whose operands take twice the registers.
+constexpr int kShapes[5][3] = {{1, 4, 2}, {2, 2, 2}, {4, 2, 1}, {8, 1, 1}, {4, 1, 1}};
 
 int variant_of(int rows, int dt) {
-  if (dt == kF32) return rows <= 32 ? 4 : 5;
-  return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3;
+  if (rows <= 32) return 0;
+  return dt == kF32 ? 4 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3;
 }
 
 Plan plan_of(const PagedView &c, int B, int T, int Hq, int dt, int cus) {
@@ -808,7 +808,7 @@ Plan plan_of(const PagedView &c, int B, int T, int Hq, int dt, int cus) {
   p.nrt = (rows + TR - 1) / TR;
   const long most = ((long)c.max_len + IK - 1) / IK;
   const long items = (long)B * p.nrt * c.Hkv * most;
-  p.W = (int)std::min<long>(items, cus);
+  p.W = (int)std::min<long>(items, (long)cus * (dt == kF32 ? 1 : sh[2]));
   p.join = most > 1 && p.W > 0;
   return p;
 }
@@ -824,14 +824,13 @@ template <typename T, typename S, int D, int V> hipError_t launch(const TreeArgs
 }
 
 template <typename T, typename S, int D> hipError_t by_rows(const TreeArgs &a, const Plan &p, hipStream_t s) {
-  if constexpr (sizeof(T) == 4) {
-    return p.variant == 4 ? launch<T, S, D, 4>(a, p, s) : launch<T, S, D, 5>(a, p, s);
-  } else {
-    return p.variant == 0   ? launch<T, S, D, 0>(a, p, s)
-           : p.variant == 1 ? launch<T, S, D, 1>(a, p, s)
+  if (p.variant == 0) return launch<T, S, D, 0>(a, p, s);
+  if constexpr (sizeof(T) == 4)
+    return launch<T, S, D, 4>(a, p, s);
+  else
+    return p.variant == 1 ? launch<T, S, D, 1>(a, p, s)
            : p.variant == 2 ? launch<T, S, D, 2>(a, p, s)
                             : launch<T, S, D, 3>(a, p, s);
-  }
 }
 
 template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Plan &p, hipStream_t s) {
