@@ -45,13 +45,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 // 8-bit row.
 constexpr int tile_keys(int RW, int D) { return RW * 1024 / D > 32 ? RW * 1024 / D : 32; }
 
-// Shape of one variant: RW waves side by side on rows, KW groups of them taking
-// tiles of TK keys in turn.
-template <typename T, int D, int RW_, int KW_> struct Shape {
-  static constexpr int RW = RW_, KW = KW_;
+// Shape of one variant: RW waves side by side on MF rows each (the side of the
+// matrix instructions' tile), KW groups of them taking tiles of TK keys in turn.
+template <typename T, int D, int MF_, int RW_, int KW_> struct Shape {
+  static constexpr int MF = MF_, RW = RW_, KW = KW_;
   static constexpr int TK = tile_keys(RW, D);
   static constexpr int IK = TK * KW;             // keys per work item
-  static constexpr int TR = 32 * RW;        // rows per tile
+  static constexpr int TR = MF * RW;        // rows per tile
   static constexpr int NT = 64 * RW * KW;        // threads
   static constexpr int NBUF = RW == 1 ? 1 : 2;   // LDS buffers per group
   static constexpr int RB = D * (int)sizeof(T);  // bytes per row in LDS
@@ -270,6 +270,34 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
 
 // ---- the kernel -------------------------------------------------------------------
 
+// The matrix instructions with tiles of MF x MF.  A step multiplies one 16-byte
+// piece of every lane's left row (lane % MF) with one of its right column; lane
+// group lane / MF of NG takes its own piece.  Register 4 q + e of a result holds
+// row 4 (NG q + lane / MF) + e of column lane % MF.
+template <int MF> struct Acc { typedef f32x16 type; };
+template <> struct Acc<16> { typedef f32x4 type; };
+template <int MF>
+__device__ __forceinline__ typename Acc<MF>::type one_mm(float a, float b, typename Acc<MF>::type c) {
+  if constexpr (MF == 32)
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+template <typename T, int MF>
+__device__ __forceinline__ typename Acc<MF>::type step_mm(const u32x4 &a, const u32x4 &b, typename Acc<MF>::type c) {
+  if constexpr (sizeof(T) == 2) {
+    if constexpr (MF == 32)
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) c = one_mm<MF>(x[w], y[w], c);
+    return c;
+  }
+}
+
 // A value that is the same in every lane, where the compiler can see it (in scalar
 // registers, and branches on it taken by the wave as a whole).
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -310,13 +338,16 @@ __device__ __forceinline__ uint32_t mask_word(const uint8_t *mp, int c, int T) {
   return d >= 4 || d <= -4 ? 0u : d >= 0 ? w >> 8 * d : w << -8 * d;
 }
 
-template <typename T, typename S, int D, int RW, int KW>
+template <typename T, typename S, int D, int MF, int RW, int KW>
 __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_attn(TreeArgs a, int nrt, int W_) {
-  using Sh = Shape<T, D, RW, KW>;
-  constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / 32;
+  using Sh = Shape<T, D, MF, RW, KW>;
+  using V = typename Acc<MF>::type;
+  constexpr int TK = Sh::TK, IK = Sh::IK, TR = Sh::TR, NT = Sh::NT, NS = TK / 32, NDT = D / MF;
+  constexpr int NG = 64 / MF, NSUB = 32 / MF;          // lane groups; tiles of 32 keys
+  constexpr int NQ = MF * MF / 256;                    // runs of 4 registers of a result
   constexpr int VPR = D * (int)sizeof(T) / 16;
-  constexpr int NC = VPR / 2;                      // steps of two 16-byte pieces along a key
-  constexpr int NPW = sizeof(T) == 2 ? 8 : 16;     // registers of 32 keys' probabilities
+  constexpr int NC = VPR / NG;                         // steps along a key
+  constexpr int NR = 32 / NG, NPW = NR * sizeof(T) / 4;  // scores of a lane's 32 keys, registers of their weights
   __shared__ __attribute__((aligned(16))) unsigned char s_mem[Sh::LDS];
   __shared__ float s_ml[KW > 1 ? KW * RW * 64 : 1][2];
   __shared__ long s_scan[NT / 64];
@@ -326,7 +357,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
   const PagedView &c = a.c;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int grp = wave / RW, rw = wave % RW;
-  const int n32 = lane & 31, h = lane >> 5;
+  const int n = lane % MF, h = lane / MF;
   const int G = a.Hq / c.Hkv, E = a.B * nrt;
   // the items of every segment, this range of them, and the segment it starts in
   Work<D> work{a.ws, 2L * W_, TR};
@@ -424,22 +455,21 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       tile.pages(c, table, kbeg, end);
       tile.load(c, table, hk, 0, kbeg, end);
     }
-    // this lane's row: node, head, and q, 16 bytes of two neighbouring pieces per
-    // step: the right operand
-    const int row = rt * TR + 32 * rw + n32, rowc = min(row, sp.live - 1);
+    // this lane's row: node, head, and q, a 16-byte piece per step: the right operand
+    const int row = rt * TR + MF * rw + n, rowc = min(row, sp.live - 1);
     const int node = rowc / G, head = hk * G + rowc % G;
     u32x4 qf[NC];
     {
       const T *qp = (const T *)a.q + ((long)b * a.T + node) * a.qs + (long)head * D;
 #pragma unroll
-      for (int cc = 0; cc < NC; ++cc) qf[cc] = *reinterpret_cast<const u32x4 *>((const char *)qp + 16 * (2 * cc + h));
+      for (int cc = 0; cc < NC; ++cc) qf[cc] = *reinterpret_cast<const u32x4 *>((const char *)qp + 16 * (NG * cc + h));
     }
-    const bool wlive = rt * TR + 32 * rw < sp.live;  // some row of this wave is there
+    const bool wlive = rt * TR + MF * rw < sp.live;  // some row of this wave is there
     const float scl = a.scale * kLog2e;
     float m = -INFINITY, l = 0.f;  // running maximum (log2 units) and sum
-    f32x16 o[NDT];
+    V o[NDT];
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x16(0.f);
+    for (int dt = 0; dt < NDT; ++dt) o[dt] = V(0.f);
     uint32_t pw[NPW];      // probabilities as the second product takes them
     uint32_t seen = ~0u;   // bit r: register r's key is seen
 
@@ -461,31 +491,28 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
     // S^T = K Q^T, then probabilities and their sum.
     auto scores = [&](int j, int u, auto kMasked) __attribute__((always_inline)) {
       const int k0 = kbeg + j * IK + 32 * u;
-      // 16-byte piece 2 cc + h of row n32: ^ 32 cc
-      const uint32_t ka = opaque(bufs_at + (j % Sh::NBUF) * Sh::BUF + 32 * u * Sh::RB + 16 * piece_at<VPR>(n32, h));
-      f32x16 s = f32x16(0.f);
+      // piece NG cc + h of row n: ^ 16 NG cc
+      const uint32_t ka = opaque(bufs_at + (j % Sh::NBUF) * Sh::BUF + 32 * u * Sh::RB + 16 * piece_at<VPR>(n, h));
+      V sv[NSUB];
 #pragma unroll
-      for (int cc = 0; cc < NC; ++cc) {
-        const u32x4 kf = lds_read<u32x4>(ka ^ (32 * cc));
-        if constexpr (sizeof(T) == 2) {
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[cc]),
-                                                      s, 0, 0, 0);
-        } else {
-          const f32x4 kv = __builtin_bit_cast(f32x4, kf), qv = __builtin_bit_cast(f32x4, qf[cc]);
+      for (int t = 0; t < NSUB; ++t) sv[t] = V(0.f);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[w], qv[w], s, 0, 0, 0);
-        }
-      }
-      // log2 units from the maximum on; register r: key k0 + 8 (r / 4) + 4 h + r % 4
+      for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+        for (int t = 0; t < NSUB; ++t)
+          sv[t] = step_mm<T, MF>(lds_read<u32x4>((ka ^ (16 * NG * cc)) + t * MF * Sh::RB), qf[cc], sv[t]);
+      // log2 units from the maximum on; score 4 q + e: key k0 + 4 (NG q + h) + e
       const float mr = m == -INFINITY ? 0.f : m;
-      s = s * scl - mr;
+      float s[NR];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) s[r] = sv[r / (4 * NQ)][r % (4 * NQ)] * scl - mr;
       if constexpr (decltype(kMasked)::value) {
         const uint8_t *mp = opaque(a.mask ? a.mask + ((size_t)b * a.T + node) * a.T : nullptr);
         const int c0 = opaque(k0 - sp.P + 4 * h);
         uint32_t sn = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // four neighbouring keys
-          const int cn = c0 + 8 * i;
+        for (int i = 0; i < NR / 4; ++i) {  // four neighbouring keys
+          const int cn = c0 + 4 * NG * i;
           const uint32_t own = mp ? mask_word(mp, cn, a.T) : 0u;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
@@ -496,11 +523,12 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
         }
         seen = sn;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = (sn >> r & 1) ? s[r] : -INFINITY;
+        for (int r = 0; r < NR; ++r) s[r] = (sn >> r & 1) ? s[r] : -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+      for (int r = 0; r < NR; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+      if constexpr (MF == 16) mx = xor16_max(mx);
       mx = xor32_max(mx);
       // the maximum is raised only when a score passes it by 2^8: probabilities
       // stay below that, and the accumulators are seldom rescaled
@@ -511,10 +539,11 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
-        s -= by;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[r] -= by;
       }
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
+      for (int r = 0; r < NR; r += 2) {
         const float p0 = __builtin_amdgcn_exp2f(s[r]), p1 = __builtin_amdgcn_exp2f(s[r + 1]);
         if constexpr (sizeof(T) == 2) {
           // the sum takes the rounded values, so the result is a weighted mean
@@ -544,7 +573,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
         // key, every row over the keys it sees
 #pragma unroll 1
         for (int key = 0; key < 32; ++key) {
-          const int hh = opaque(h), r0 = (key >> 3) * 4 + (key & 3), from = n32 + 32 * (key >> 2 & 1);
+          const int hh = opaque(h), r0 = key / (4 * NG) * 4 + (key & 3), from = n + MF * (key / 4 % NG);
           uint32_t w = 0;
 #pragma unroll
           for (int r = 0; r < NPW; ++r)
@@ -557,8 +586,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
 #pragma unroll
-            for (int g8 = 0; g8 < 4; ++g8) {
-              const int by = (32 * dt + 8 * g8 + 4 * hh) * (int)sizeof(T);
+            for (int g8 = 0; g8 < NQ; ++g8) {
+              const int by = (MF * dt + 4 * (NG * g8 + hh)) * (int)sizeof(T);
               const uint32_t va = vb + 16 * piece_at<VPR>(key, by / 16) + by % 16;
               f32x4 vw;
               if constexpr (sizeof(T) == 2) {
@@ -578,32 +607,31 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
         return;
       }
       if constexpr (sizeof(T) == 2) {
-        // keys 8 i + 4 h + 0 .. 3 (i even) and the same 8 further, dim 32 dt + n32: the
-        // transposing read (lane 4 e + q of 16 names key e, dims 4 q .. + 3); the dims
-        // of step dt lie ^ 64 dt
-        const int R = 4 * h + (lane >> 2 & 3), pc = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        // keys 4 (NG i + h) + 0 .. 3 and those of i + 1, dim MF dt + n: the transposing
+        // read (lane 4 e + d of 16 names key e, dims 4 d .. + 3, and gets dim lane % 16
+        // of the four keys); the dims of step dt lie ^ 2 MF dt
+        const int R = 4 * h + (lane >> 2 & 3), pc = (MF == 32 ? 2 * (lane >> 4 & 1) : 0) + (lane >> 1 & 1);
         const uint32_t va0 = opaque(vb + 16 * piece_at<VPR>(R, pc) + 8 * (lane & 1));
-        const uint32_t va1 = opaque(vb + 16 * piece_at<VPR>(R + 8, pc) + 8 * (lane & 1));
+        const uint32_t va1 = opaque(vb + 16 * piece_at<VPR>(R + 4 * NG, pc) + 8 * (lane & 1));
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) {
+        for (int i = 0; i < NR / 4; i += 2) {
           const u32x4 pf = {pw[2 * i], pw[2 * i + 1], pw[2 * i + 2], pw[2 * i + 3]};
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
-            const u32x2 v0 = lds_read_tr((va0 ^ (64 * dt)) + 8 * i * Sh::RB);
-            const u32x2 v1 = lds_read_tr((va1 ^ (64 * dt)) + 8 * i * Sh::RB);
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, (u32x4{v0.x, v0.y, v1.x, v1.y})),
-                                                            __builtin_bit_cast(bf16x8, pf), o[dt], 0, 0, 0);
+            const u32x2 v0 = lds_read_tr((va0 ^ (2 * MF * dt)) + 4 * NG * i * Sh::RB);
+            const u32x2 v1 = lds_read_tr((va1 ^ (2 * MF * dt)) + 4 * NG * i * Sh::RB);
+            o[dt] = step_mm<T, MF>(u32x4{v0.x, v0.y, v1.x, v1.y}, pf, o[dt]);
           }
         }
       } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 8 * (r / 4) + 4 * h + r % 4;
+        for (int r = 0; r < NR; ++r) {
+          const int key = 4 * (NG * (r / 4) + h) + r % 4;
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
-            const int by = 4 * (32 * dt + n32);
+            const int by = 4 * (MF * dt + n);
             const float vf = lds_read<float>(vb + 16 * piece_at<VPR>(key, by / 16) + by % 16);
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, __uint_as_float(pw[r]), o[dt], 0, 0, 0);
+            o[dt] = one_mm<MF>(vf, __uint_as_float(pw[r]), o[dt]);
           }
         }
       }
@@ -634,20 +662,21 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
     for (int j = 0; j < jm; ++j) step(j, std::false_type{});
 #pragma unroll 1
     for (int j = jm; j < nj; ++j) step(j, std::true_type{});
+    if constexpr (MF == 16) l = xor16_sum(l);
     l = xor32_sum(l);
 
     // groups add up: group g > 0 leaves its sums in LDS, group 0 takes them in order
     if constexpr (KW > 1) {
-      f32x4 *so = reinterpret_cast<f32x4 *>(s_mem);  // [(KW - 1) RW][D / 8][64]
-      static_assert((KW - 1) * RW * (D / 8) * 64 * 16 <= Sh::LDS, "sums fit the tiles' buffers");
+      f32x4 *so = reinterpret_cast<f32x4 *>(s_mem);  // [(KW - 1) RW][NDT NQ][64]
+      static_assert((KW - 1) * RW * NDT * NQ * 64 * 16 <= Sh::LDS, "sums fit the tiles' buffers");
       __syncthreads();
       if (grp > 0) {
         const int at_w = (grp - 1) * RW + rw;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-          for (int g8 = 0; g8 < 4; ++g8)
-            so[(at_w * (D / 8) + 4 * dt + g8) * 64 + lane] =
+          for (int g8 = 0; g8 < NQ; ++g8)
+            so[(at_w * NDT * NQ + NQ * dt + g8) * 64 + lane] =
                 f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
         s_ml[at_w * 64 + lane][0] = m;
         s_ml[at_w * 64 + lane][1] = l;
@@ -669,8 +698,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-            for (int g8 = 0; g8 < 4; ++g8) {
-              const f32x4 w = so[(at_w * (D / 8) + 4 * dt + g8) * 64 + lane];
+            for (int g8 = 0; g8 < NQ; ++g8) {
+              const f32x4 w = so[(at_w * NDT * NQ + NQ * dt + g8) * 64 + lane];
 #pragma unroll
               for (int w4 = 0; w4 < 4; ++w4) o[dt][4 * g8 + w4] += w[w4] * scg;
             }
@@ -685,22 +714,22 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-          for (int g8 = 0; g8 < 4; ++g8) {
+          for (int g8 = 0; g8 < NQ; ++g8) {
             const f32x4 w = f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]} * inv;
             if constexpr (sizeof(T) == 2)
-              *reinterpret_cast<u32x2 *>(op + 32 * dt + 8 * g8) = u32x2{f2bf2(w.x, w.y), f2bf2(w.z, w.w)};
+              *reinterpret_cast<u32x2 *>(op + MF * dt + 4 * NG * g8) = u32x2{f2bf2(w.x, w.y), f2bf2(w.z, w.w)};
             else
-              *reinterpret_cast<f32x4 *>(op + 32 * dt + 8 * g8) = w;
+              *reinterpret_cast<f32x4 *>(op + MF * dt + 4 * NG * g8) = w;
           }
       } else {
         const long slot = 2L * wg + (i0 > 0 ? 0 : 1);
-        const int rr = 32 * rw + n32;
+        const int rr = MF * rw + n;
         float *po = work.o(slot) + (long)rr * D + 4 * h;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-          for (int g8 = 0; g8 < 4; ++g8)
-            *reinterpret_cast<f32x4 *>(po + 32 * dt + 8 * g8) =
+          for (int g8 = 0; g8 < NQ; ++g8)
+            *reinterpret_cast<f32x4 *>(po + MF * dt + 4 * NG * g8) =
                 f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
         if (h == 0) *reinterpret_cast<float2 *>(work.ml(slot) + 2 * rr) = float2{m, l};
       }
@@ -790,13 +819,13 @@ struct Plan {
 };
 constexpr int kMaxCus = 512;
 
-// Variants by rows per (sequence, KV head): RW, KW, workgroups per compute unit.
+// Variants by rows per (sequence, KV head): MF, RW, KW, workgroups per compute unit.
 // The last is fp32's, whose operands take twice the registers.
-constexpr int kShapes[5][3] = {{1, 4, 2}, {2, 2, 2}, {4, 2, 1}, {8, 1, 1}, {4, 1, 1}};
+constexpr int kShapes[6][4] = {{16, 1, 4, 2}, {32, 1, 4, 2}, {32, 2, 2, 2}, {32, 4, 2, 1}, {32, 8, 1, 1}, {32, 4, 1, 1}};
 
 int variant_of(int rows, int dt) {
-  if (rows <= 32) return 0;
-  return dt == kF32 ? 4 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3;
+  if (rows <= 16) return 0;
+  return dt == kF32 ? 5 : rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 3 : 4;
 }
 
 Plan plan_of(const PagedView &c, int B, int T, int Hq, int dt, int cus) {
@@ -804,18 +833,18 @@ Plan plan_of(const PagedView &c, int B, int T, int Hq, int dt, int cus) {
   Plan p;
   p.variant = variant_of(rows, dt);
   const int *sh = kShapes[p.variant];
-  const int TR = 32 * sh[0], IK = sh[1] * tile_keys(sh[0], c.D);
+  const int TR = sh[0] * sh[1], IK = sh[2] * tile_keys(sh[1], c.D);
   p.nrt = (rows + TR - 1) / TR;
   const long most = ((long)c.max_len + IK - 1) / IK;
   const long items = (long)B * p.nrt * c.Hkv * most;
-  p.W = (int)std::min<long>(items, (long)cus * (dt == kF32 ? 1 : sh[2]));
+  p.W = (int)std::min<long>(items, (long)cus * (dt == kF32 ? 1 : sh[3]));
   p.join = most > 1 && p.W > 0;
   return p;
 }
 
 template <typename T, typename S, int D, int V> hipError_t launch(const TreeArgs &a, const Plan &p, hipStream_t s) {
-  using Sh = Shape<T, D, kShapes[V][0], kShapes[V][1]>;
-  k_tree_attn<T, S, D, Sh::RW, Sh::KW><<<p.W, Sh::NT, 0, s>>>(a, p.nrt, p.W);
+  using Sh = Shape<T, D, kShapes[V][0], kShapes[V][1], kShapes[V][2]>;
+  k_tree_attn<T, S, D, Sh::MF, Sh::RW, Sh::KW><<<p.W, Sh::NT, 0, s>>>(a, p.nrt, p.W);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.join) return e;
   const int rows = std::min<long>(Sh::TR, (long)a.T * (a.Hq / a.c.Hkv));
@@ -826,11 +855,12 @@ template <typename T, typename S, int D, int V> hipError_t launch(const TreeArgs
 template <typename T, typename S, int D> hipError_t by_rows(const TreeArgs &a, const Plan &p, hipStream_t s) {
   if (p.variant == 0) return launch<T, S, D, 0>(a, p, s);
   if constexpr (sizeof(T) == 4)
-    return launch<T, S, D, 4>(a, p, s);
+    return launch<T, S, D, 5>(a, p, s);
   else
-    return p.variant == 1 ? launch<T, S, D, 1>(a, p, s)
+    return p.variant == 1   ? launch<T, S, D, 1>(a, p, s)
            : p.variant == 2 ? launch<T, S, D, 2>(a, p, s)
-                            : launch<T, S, D, 3>(a, p, s);
+           : p.variant == 3 ? launch<T, S, D, 3>(a, p, s)
+                            : launch<T, S, D, 4>(a, p, s);
 }
 
 template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Plan &p, hipStream_t s) {
@@ -841,7 +871,7 @@ template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Pla
 
 size_t tree_attention_ws(const PagedView &c, int B, int T, int Hq, int dt) {
   const Plan p = plan_of(c, B, T, Hq, dt, kMaxCus);
-  const size_t rows = 2 * (size_t)p.W * 32 * kShapes[p.variant][0];
+  const size_t rows = 2 * (size_t)p.W * kShapes[p.variant][0] * kShapes[p.variant][1];
   return (rows * (c.D + 2) * 4 + ((size_t)B * p.nrt + 1) * 8 + 255) & ~(size_t)255;
 }
 
