@@ -514,7 +514,7 @@ fe_status fe_test_attn_split(const int32_t *prefix_lens, int32_t batch, int32_t 
 typedef struct {
   void *k, *v;        /* [n_pages * page_rows, H_kv, D] in dtype, 16-byte aligned */
   uint8_t *k_scale, *v_scale; /* FE_F8 only, else ignored: [H_kv, n_pages * page_rows], 4-byte aligned */
-  int32_t n_pages;
+  int32_t n_pages;    /* n_pages * page_rows below 2^31 */
   int32_t page_rows;  /* a power of two, 16 .. 65536 */
   int32_t n_kv_heads; /* 1 .. 256 */
   int32_t head_dim;   /* 64 or 128 */

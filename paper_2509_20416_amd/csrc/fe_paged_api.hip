@@ -22,6 +22,7 @@ fe_status check_cache(const fe_paged_kv *c) {
     return fail(FE_E_INVALID, "cache has a non-positive size");
   if (c->page_rows < 16 || c->page_rows > 65536 || (c->page_rows & (c->page_rows - 1)))
     return fail(FE_E_UNSUPPORTED, "page_rows must be a power of two, 16 .. 65536");
+  if ((int64_t)c->n_pages * c->page_rows > INT32_MAX) return fail(FE_E_UNSUPPORTED, "the pool has more than 2^31 - 1 rows");
   if (c->n_kv_heads > 256) return fail(FE_E_UNSUPPORTED, "n_kv_heads > 256");
   if (c->head_dim != 64 && c->head_dim != 128) return fail(FE_E_UNSUPPORTED, "head_dim must be 64 or 128");
   if (!c->k || !c->v) return fail(FE_E_INVALID, "cache keys or values are NULL");

@@ -155,9 +155,9 @@ template <int VPR> __device__ __forceinline__ int piece_at(int R, int p) {
 }
 
 // A wave's rows in one load are at most 16 neighbours (and a page holds whole runs
-// of 16), so the page and the row's address are wave-uniform: the ids of the next
-// 1024 keys' pages sit in one register, a lane per 16 keys, and each load picks its
-// own with a readlane.
+// of 16), so their address is wave-uniform: the rows that the runs of the next 1024
+// keys start at sit in one register, a lane per run, and each load picks its own
+// with a readlane.
 template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
   static constexpr int PS = D * (int)sizeof(S) / 16;  // 16-byte pieces of a stored row
   static constexpr int VPR = D * (int)sizeof(T) / 16;
@@ -165,53 +165,55 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
   static constexpr int STEP = RW * SPAN;              // rows between a thread's loads
   static constexpr int NL = TK / STEP;                // loads per thread, K (as many V)
   static_assert(SPAN >= 1 && SPAN <= 16 && NL >= 1 && TK % STEP == 0, "whole loads inside runs of 16 rows");
-  static constexpr int WIN = 1024 / IK;               // tiles per register of page ids
+  static constexpr int WIN = 1024 / IK;               // tiles per register of runs
   static constexpr bool F8 = sizeof(S) == 1;
   u32x4 k[NL], v[NL];
   uint32_t sk[NL], sv[NL];  // scale bytes
-  int pid, pid_next;        // lane l: page of keys 16 l .. + 15 of this window, of the next
+  int run, run_next;        // lane l: first row of keys 16 l .. + 15 of this window, of the next; -1: a bad page
   uint32_t badp;            // bit i: load i's page lies outside the pool
   int rw, lrow, lpc;        // this wave; this lane's row and piece in its load
-  uint32_t loff;
+  uint32_t loff, rowb;
 
   __device__ __forceinline__ void init(const PagedView &c, int rw_, int lane) {
     rw = rw_;
     lrow = lane / PS;
     lpc = lane % PS;
-    loff = lrow * (uint32_t)(c.Hkv * D * sizeof(S)) + 16 * lpc;
+    rowb = c.Hkv * D * (int)sizeof(S);
+    loff = lrow * rowb + 16 * lpc;
   }
   __device__ __forceinline__ int row(int i) const { return i * STEP + rw * SPAN + lrow; }
-  __device__ __forceinline__ static int ids(const PagedView &c, const int32_t *table, int w0, int end) {
-    return table[min(w0 + 16 * (int)(threadIdx.x & 63), end - 1) >> c.shift];
+  __device__ __forceinline__ static int runs(const PagedView &c, const int32_t *table, int w0, int end) {
+    const int pos = min(w0 + 16 * (int)(threadIdx.x & 63), (end - 1) & ~15);
+    const int pg = table[pos >> c.shift];
+    return (unsigned)pg < (unsigned)c.n_pages ? (pg << c.shift) + (pos & ((1 << c.shift) - 1)) : -1;
   }
   // The first two windows of a run of tiles that starts at key k0.
   __device__ __forceinline__ void pages(const PagedView &c, const int32_t *table, int k0, int end) {
-    pid = ids(c, table, k0, end);
-    pid_next = ids(c, table, min(k0 + 1024, end), end);
+    run = runs(c, table, k0, end);
+    run_next = runs(c, table, min(k0 + 1024, end), end);
   }
   // Loads tile j of the run (keys k0 ..); rows past end are some row of a page that
   // belongs to the sequence.
   __device__ __forceinline__ void load(const PagedView &c, const int32_t *table, int hk, int j, int k0, int end) {
     if (j > 0 && j % WIN == 0) {
-      pid = pid_next;
-      pid_next = ids(c, table, min(k0 + 1024, end), end);
+      run = run_next;
+      run_next = runs(c, table, min(k0 + 1024, end), end);
     }
     badp = 0;
-    const uint32_t rowb = c.Hkv * D * sizeof(S);
+    const char *kb = (const char *)c.k + hk * (D * (int)sizeof(S)), *vb = (const char *)c.v + hk * (D * (int)sizeof(S));
 #pragma unroll
-    for (int q = 0; q < 2 * NL; ++q) {                  // K's loads, then V's
-      const int i = q % NL, R0 = i * STEP + rw * SPAN;  // uniform
-      const int pg = __builtin_amdgcn_readlane(pid, (j % WIN * IK + R0) / 16);
-      const bool ok = (unsigned)pg < (unsigned)c.n_pages;
-      if (!ok) badp |= 1u << i;
-      const long r = ((long)(ok ? pg : 0) << c.shift) + ((k0 + R0) & ((1 << c.shift) - 1));
-      const long at = r * rowb + hk * (D * (int)sizeof(S));
-      const u32x4 w = *reinterpret_cast<const u32x4 *>((const char *)(q < NL ? c.k : c.v) + at + loff);
-      if (q < NL)
-        k[i] = w;
-      else
-        v[i] = w;
-      if constexpr (F8) (q < NL ? sk : sv)[i] = ((q < NL ? c.ks : c.vs) + hk * c.rows() + r)[(uint32_t)lrow];
+    for (int i = 0; i < NL; ++i) {
+      const int R0 = i * STEP + rw * SPAN;  // uniform
+      const int first = __builtin_amdgcn_readlane(run, (j % WIN * IK + R0) / 16);
+      if (first < 0) badp |= 1u << i;
+      const uint32_t r = (uint32_t)max(first, 0) + R0 % 16;
+      const uint64_t at = (uint64_t)r * rowb;
+      k[i] = *reinterpret_cast<const u32x4 *>(kb + at + loff);
+      v[i] = *reinterpret_cast<const u32x4 *>(vb + at + loff);
+      if constexpr (F8) {
+        sk[i] = (c.ks + hk * c.rows() + r)[(uint32_t)lrow];
+        sv[i] = (c.vs + hk * c.rows() + r)[(uint32_t)lrow];
+      }
     }
   }
   __device__ __forceinline__ static void put(unsigned char *lds, int R, int p, const u32x4 &w, uint32_t s) {
@@ -233,20 +235,20 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
       }
     }
   }
-  // Writes the tile; ragged: rows from `left` on become zeros.  A row on a bad page
-  // becomes NaN keys (and zero values).  Returns whether a value this thread wrote
-  // is not finite (asked for masked tiles only).
+  // Writes the tile.  masked: rows from `left` on become zeros, a row on a bad page
+  // NaN keys (and zero values); returns whether a value this thread wrote is not
+  // finite.
   template <bool masked> __device__ __forceinline__ bool store(unsigned char *lds, int left) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int R = row(i);
       u32x4 kw = k[i], vw = v[i];
-      if (badp >> i & 1) {
-        kw = u32x4(0xffffffffu);
-        vw = u32x4(0u);
-      }
       if constexpr (masked) {
+        if (badp >> i & 1) {
+          kw = u32x4(0xffffffffu);
+          vw = u32x4(0u);
+        }
         if (R >= left) kw = vw = u32x4(0u);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -471,6 +473,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = V(0.f);
     uint32_t pw[NPW];      // probabilities as the second product takes them
+    u32x2 vf[NR / 8 * NDT][2];  // bf16: values of 32 keys
     uint32_t seen = ~0u;   // bit r: register r's key is seen
 
     // Tile j + 1 into its buffer, between barriers j and j + 1: tile j - 1's readers
@@ -480,12 +483,12 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
     auto put = [&](int j) __attribute__((always_inline)) {
       const int k0 = kbeg + j * IK, at_buf = j % Sh::NBUF;
       unsigned char *kb = bufs + at_buf * Sh::BUF;
-      if (k0 + TK > vis_all) {
+      if (k0 + TK > vis_all || tile.badp != 0) {
         const bool odd = __builtin_amdgcn_ballot_w64(tile.template store<true>(kb, end - k0)) != 0;
         if (RW > 1 && lane == 0) s_odd[at_buf][wave] = odd;
         odd_own = (odd_own & ~(1u << at_buf)) | (uint32_t)odd << at_buf;
       } else {
-        tile.template store<false>(kb, TK);
+        tile.template store<false>(kb, 0);
       }
     };
     // S^T = K Q^T, then probabilities and their sum.
@@ -496,11 +499,42 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       V sv[NSUB];
 #pragma unroll
       for (int t = 0; t < NSUB; ++t) sv[t] = V(0.f);
+      // reads first, eight at a time: left to itself the compiler reads into one set
+      // of registers and waits out the LDS before every product
+      constexpr int KB = NC * NSUB < 8 ? NC * NSUB : 8;
 #pragma unroll
-      for (int cc = 0; cc < NC; ++cc)
+      for (int c0 = 0; c0 < NC * NSUB; c0 += KB) {
+        u32x4 kf[KB];
 #pragma unroll
-        for (int t = 0; t < NSUB; ++t)
-          sv[t] = step_mm<T, MF>(lds_read<u32x4>((ka ^ (16 * NG * cc)) + t * MF * Sh::RB), qf[cc], sv[t]);
+        for (int i = 0; i < KB; ++i) {
+          const int cc = (c0 + i) / NSUB, t = (c0 + i) % NSUB;
+          kf[i] = lds_read<u32x4>((ka ^ (16 * NG * cc)) + t * MF * Sh::RB);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {
+          const int cc = (c0 + i) / NSUB, t = (c0 + i) % NSUB;
+          sv[t] = step_mm<T, MF>(kf[i], qf[cc], sv[t]);
+        }
+      }
+      if constexpr (sizeof(T) == 2) {
+        // the values' reads go out before the scores are worked on.
+        // Keys 4 (NG i + h) + 0 .. 3 and those of i + 1, dim MF dt + n: the transposing
+        // read (lane 4 e + d of 16 names key e, dims 4 d .. + 3, and gets dim lane % 16
+        // of the four keys); the dims of step dt lie ^ 2 MF dt
+        const uint32_t vb = bufs_at + (j % Sh::NBUF) * Sh::BUF + (TK + 32 * u) * Sh::RB;
+        const int R = 4 * h + (lane >> 2 & 3), pc = (MF == 32 ? 2 * (lane >> 4 & 1) : 0) + (lane >> 1 & 1);
+        const uint32_t va0 = opaque(vb + 16 * piece_at<VPR>(R, pc) + 8 * (lane & 1));
+        const uint32_t va1 = opaque(vb + 16 * piece_at<VPR>(R + 4 * NG, pc) + 8 * (lane & 1));
+#pragma unroll
+        for (int i = 0; i < NR / 4; i += 2)
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            vf[i / 2 * NDT + dt][0] = lds_read_tr((va0 ^ (2 * MF * dt)) + 4 * NG * i * Sh::RB);
+            vf[i / 2 * NDT + dt][1] = lds_read_tr((va1 ^ (2 * MF * dt)) + 4 * NG * i * Sh::RB);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
       // log2 units from the maximum on; score 4 q + e: key k0 + 4 (NG q + h) + e
       const float mr = m == -INFINITY ? 0.f : m;
       float s[NR];
@@ -607,19 +641,12 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
         return;
       }
       if constexpr (sizeof(T) == 2) {
-        // keys 4 (NG i + h) + 0 .. 3 and those of i + 1, dim MF dt + n: the transposing
-        // read (lane 4 e + d of 16 names key e, dims 4 d .. + 3, and gets dim lane % 16
-        // of the four keys); the dims of step dt lie ^ 2 MF dt
-        const int R = 4 * h + (lane >> 2 & 3), pc = (MF == 32 ? 2 * (lane >> 4 & 1) : 0) + (lane >> 1 & 1);
-        const uint32_t va0 = opaque(vb + 16 * piece_at<VPR>(R, pc) + 8 * (lane & 1));
-        const uint32_t va1 = opaque(vb + 16 * piece_at<VPR>(R + 4 * NG, pc) + 8 * (lane & 1));
 #pragma unroll
         for (int i = 0; i < NR / 4; i += 2) {
           const u32x4 pf = {pw[2 * i], pw[2 * i + 1], pw[2 * i + 2], pw[2 * i + 3]};
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
-            const u32x2 v0 = lds_read_tr((va0 ^ (2 * MF * dt)) + 4 * NG * i * Sh::RB);
-            const u32x2 v1 = lds_read_tr((va1 ^ (2 * MF * dt)) + 4 * NG * i * Sh::RB);
+            const u32x2 v0 = vf[i / 2 * NDT + dt][0], v1 = vf[i / 2 * NDT + dt][1];
             o[dt] = step_mm<T, MF>(u32x4{v0.x, v0.y, v1.x, v1.y}, pf, o[dt]);
           }
         }

@@ -35,7 +35,7 @@ BAD_CACHE = [
     (dict(dtype=3), "FE_E_INVALID"), (dict(n_pages=0), "FE_E_INVALID"), (dict(n_kv_heads=0), "FE_E_INVALID"),
     (dict(page_rows=0), "FE_E_INVALID"), (dict(page_rows=48), "FE_E_UNSUPPORTED"),
     (dict(page_rows=8), "FE_E_UNSUPPORTED"), (dict(page_rows=1 << 17), "FE_E_UNSUPPORTED"),
-    (dict(n_kv_heads=257), "FE_E_UNSUPPORTED"), (dict(head_dim=96), "FE_E_UNSUPPORTED"),
+    (dict(n_kv_heads=257), "FE_E_UNSUPPORTED"), (dict(n_pages=1 << 26), "FE_E_UNSUPPORTED"), (dict(head_dim=96), "FE_E_UNSUPPORTED"),
     (dict(k=None), "FE_E_INVALID"), (dict(v=A[1] + 8), "FE_E_ALIGN"), (dict(k_scale=None), "FE_E_INVALID"),
     (dict(v_scale=A[3] + 2), "FE_E_ALIGN"),
 ]
