@@ -58,6 +58,16 @@ template <> __device__ __forceinline__ f32x8 load8<uint8_t>(const uint8_t *p) {
   const f32x4 a = f8x4_to_f(w.x), b = f8x4_to_f(w.y);
   return f32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
+template <typename T> __device__ __forceinline__ f32x4 load4(const T *p);
+template <> __device__ __forceinline__ f32x4 load4<float>(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+template <> __device__ __forceinline__ f32x4 load4<uint16_t>(const uint16_t *p) {
+  const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+  return f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+               __uint_as_float(w.y & 0xffff0000u)};
+}
+template <> __device__ __forceinline__ f32x4 load4<uint8_t>(const uint8_t *p) {
+  return f8x4_to_f(*reinterpret_cast<const uint32_t *>(p));
+}
 template <typename T> __device__ __forceinline__ void store8(T *p, const f32x8 &f);
 template <> __device__ __forceinline__ void store8<float>(float *p, const f32x8 &f) {
   *reinterpret_cast<f32x4 *>(p) = f32x4{f[0], f[1], f[2], f[3]};

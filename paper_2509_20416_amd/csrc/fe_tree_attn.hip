@@ -29,7 +29,6 @@
 //    holds one is added key by key, each row over the keys it sees.
 #include <algorithm>
 #include <atomic>
-#include <type_traits>
 
 #include "fe_attn_unit.h"
 #include "fe_paged.h"
@@ -58,6 +57,34 @@ template <typename T, int D, int MF_, int RW_, int KW_> struct Shape {
   static constexpr int BUF = 2 * TK * RB;        // K rows, then V rows
   static constexpr int LDS = KW * NBUF * BUF;
 };
+
+// A value that is the same in every lane, where the compiler can see it (in scalar
+// registers, and branches on it taken by the wave as a whole).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long uniform(long x) {
+  return (long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
+// A value the compiler cannot compute ahead of a seldom taken branch, so that the
+// branch's addresses hold no registers outside it.
+template <typename V> __device__ __forceinline__ V opaque(V x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+template <typename V> __device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(__attribute__((address_space(3))) const V *)(uintptr_t)at;
+}
+__device__ __forceinline__ void lds_write(uint32_t at, const u32x4 &w) {
+  *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)at = w;
+}
+__device__ __forceinline__ u32x2 lds_read_tr(uint32_t at) {
+  return __builtin_bit_cast(
+      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(uintptr_t)at));
+}
 
 // ---- the split ------------------------------------------------------------------
 
@@ -90,11 +117,8 @@ __device__ __forceinline__ int keys_end(const TreeArgs &a, const Span &s, int rt
 constexpr int kSegItems = 3;
 
 // Work items of a segment: steps over its keys (none where the tile has no row).
-__device__ __forceinline__ int items_of(const TreeArgs &a, int e, int nrt, int TR, int IK) {
-  const Span s = span_of(a, e / nrt);
-  const int rt = e % nrt;
-  if (rt * TR >= s.live) return 0;
-  return max(1, (keys_end(a, s, rt, TR) + IK - 1) / IK);
+__device__ __forceinline__ int items_of(const TreeArgs &a, const Span &s, int rt, int TR, int IK) {
+  return rt * TR >= s.live ? 0 : max(1, (keys_end(a, s, rt, TR) + IK - 1) / IK);
 }
 
 // Sums of a wave's values up to each lane (below 2^32: an item count is at most 2^25).
@@ -169,6 +193,7 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
   static constexpr bool F8 = sizeof(S) == 1;
   u32x4 k[NL], v[NL];
   uint32_t sk[NL], sv[NL];  // scale bytes
+  int window;               // which 1024 keys of the run of tiles `run` is for
   int run, run_next;        // lane l: first row of keys 16 l .. + 15 of this window, of the next; -1: a bad page
   uint32_t badp;            // bit i: load i's page lies outside the pool
   int rw, lrow, lpc;        // this wave; this lane's row and piece in its load
@@ -183,21 +208,26 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
   }
   __device__ __forceinline__ int row(int i) const { return i * STEP + rw * SPAN + lrow; }
   __device__ __forceinline__ static int runs(const PagedView &c, const int32_t *table, int w0, int end) {
-    const int pos = min(w0 + 16 * (int)(threadIdx.x & 63), (end - 1) & ~15);
+    return runs1(c, table, min(w0 + 16 * (int)(threadIdx.x & 63), (end - 1) & ~15));
+  }
+  // The row of position pos; -1 on a bad page.
+  __device__ __forceinline__ static int runs1(const PagedView &c, const int32_t *table, int pos) {
     const int pg = table[pos >> c.shift];
     return (unsigned)pg < (unsigned)c.n_pages ? (pg << c.shift) + (pos & ((1 << c.shift) - 1)) : -1;
   }
   // The first two windows of a run of tiles that starts at key k0.
   __device__ __forceinline__ void pages(const PagedView &c, const int32_t *table, int k0, int end) {
+    window = 0;
     run = runs(c, table, k0, end);
     run_next = runs(c, table, min(k0 + 1024, end), end);
   }
   // Loads tile j of the run (keys k0 ..); rows past end are some row of a page that
   // belongs to the sequence.
   __device__ __forceinline__ void load(const PagedView &c, const int32_t *table, int hk, int j, int k0, int end) {
-    if (j > 0 && j % WIN == 0) {
+    if (j / WIN != window) {
+      window = j / WIN;
       run = run_next;
-      run_next = runs(c, table, min(k0 + 1024, end), end);
+      run_next = runs(c, table, min(k0 - j % WIN * IK + 1024, end), end);
     }
     badp = 0;
     const char *kb = (const char *)c.k + hk * (D * (int)sizeof(S)), *vb = (const char *)c.v + hk * (D * (int)sizeof(S));
@@ -216,21 +246,22 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
       }
     }
   }
-  __device__ __forceinline__ static void put(unsigned char *lds, int R, int p, const u32x4 &w, uint32_t s) {
-    u32x4 *dst = reinterpret_cast<u32x4 *>(lds);
+  // Load i's piece to LDS, `at` being where load 0's goes: the rows between them
+  // only add bits to the row's number, so the permutation is ^ a constant.
+  __device__ __forceinline__ static void put(uint32_t at, int i, const u32x4 &w, uint32_t s) {
+    const uint32_t to = (at ^ (16 * (piece_at<VPR>(i * STEP, 0) - i * STEP * VPR))) + i * STEP * VPR * 16;
     if constexpr (!F8) {
-      dst[piece_at<VPR>(R, p)] = w;
+      lds_write(to, w);
     } else {
       const float sc = scale_of(s);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const uint32_t a = w[2 * q], b = w[2 * q + 1];
         if constexpr (sizeof(T) == 2) {
-          dst[piece_at<VPR>(R, 2 * p + q)] = u32x4{f8_bf16<false>(a, sc), f8_bf16<true>(a, sc),
-                                                   f8_bf16<false>(b, sc), f8_bf16<true>(b, sc)};
+          lds_write(to ^ (16 * q), u32x4{f8_bf16<false>(a, sc), f8_bf16<true>(a, sc), f8_bf16<false>(b, sc), f8_bf16<true>(b, sc)});
         } else {
-          dst[piece_at<VPR>(R, 4 * p + 2 * q)] = __builtin_bit_cast(u32x4, f8x4_to_f(a) * sc);
-          dst[piece_at<VPR>(R, 4 * p + 2 * q + 1)] = __builtin_bit_cast(u32x4, f8x4_to_f(b) * sc);
+          lds_write(to ^ (32 * q), __builtin_bit_cast(u32x4, f8x4_to_f(a) * sc));
+          lds_write(to ^ (32 * q + 16), __builtin_bit_cast(u32x4, f8x4_to_f(b) * sc));
         }
       }
     }
@@ -238,7 +269,8 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
   // Writes the tile.  masked: rows from `left` on become zeros, a row on a bad page
   // NaN keys (and zero values); returns whether a value this thread wrote is not
   // finite.
-  template <bool masked> __device__ __forceinline__ bool store(unsigned char *lds, int left) {
+  template <bool masked> __device__ __forceinline__ bool store(uint32_t lds, int left) {
+    const uint32_t at = opaque(lds + 16 * piece_at<VPR>(row(0), lpc * (int)(sizeof(T) / sizeof(S))));
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -263,8 +295,8 @@ template <typename T, typename S, int D, int RW, int TK, int IK> struct Tile {
           }
         }
       }
-      put(lds, R, lpc, kw, F8 ? sk[i] : 0);
-      put(lds + TK * D * sizeof(T), R, lpc, vw, F8 ? sv[i] : 0);
+      put(at, i, kw, F8 ? sk[i] : 0);
+      put(at + TK * D * (int)sizeof(T), i, vw, F8 ? sv[i] : 0);
     }
     return odd;
   }
@@ -298,31 +330,6 @@ __device__ __forceinline__ typename Acc<MF>::type step_mm(const u32x4 &a, const 
     for (int w = 0; w < 4; ++w) c = one_mm<MF>(x[w], y[w], c);
     return c;
   }
-}
-
-// A value that is the same in every lane, where the compiler can see it (in scalar
-// registers, and branches on it taken by the wave as a whole).
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long uniform(long x) {
-  return (long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
-}
-
-// A value the compiler cannot compute ahead of a seldom taken branch, so that the
-// branch's addresses hold no registers outside it.
-template <typename V> __device__ __forceinline__ V opaque(V x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
-__device__ __forceinline__ uint32_t lds_address(const void *p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
-}
-template <typename V> __device__ __forceinline__ V lds_read(uint32_t at) {
-  return *(__attribute__((address_space(3))) const V *)(uintptr_t)at;
-}
-__device__ __forceinline__ u32x2 lds_read_tr(uint32_t at) {
-  return __builtin_bit_cast(
-      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(uintptr_t)at));
 }
 
 // Bytes c .. c + 3 of a mask row of T: one (unaligned) load where T >= 4, moved
@@ -368,7 +375,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
   uint32_t mine = 0;
   // The counts of NT entries, added to the running sums.
   auto count = [&](int e0, long &sum, int &nseg) __attribute__((always_inline)) {
-    mine = e0 + tid < E ? items_of(a, e0 + tid, nrt, TR, IK) : 0;
+    const int e = e0 + tid;
+    mine = e < E ? items_of(a, span_of(a, e / nrt), e % nrt, TR, IK) : 0;
     const uint32_t inc = wave_incl_scan(mine);
     const uint64_t some = __builtin_amdgcn_ballot_w64(mine > 0);
     if (lane == 63) {
@@ -428,7 +436,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
   }
   if (blockIdx.x == 0 && tid == 0) work.before()[E] = rg.total / c.Hkv;
   __syncthreads();
-  Tile<T, S, D, RW, TK, IK> tile;
+  typedef Tile<T, S, D, RW, TK, IK> Loads;
+  Loads tile;  // the next keys, on their way to LDS
   tile.init(c, rw, lane);
   int e = (int)uniform(s_first[0]);
   long at = uniform(s_first[1]);  // first item of entry e
@@ -436,27 +445,25 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
   const uint32_t bufs_at = lds_address(bufs);
 
   for (long x = x0; x < x1;) {
-    const int steps = items_of(a, e, nrt, TR, IK), it = steps > 0 ? steps + extra : 0;
+    const int b = e / nrt, rt = e % nrt;
+    const Span sp = span_of(a, b);
+    const int steps = items_of(a, sp, rt, TR, IK), it = steps > 0 ? steps + extra : 0;
     if (it == 0 || x >= at + (long)it * c.Hkv) {
       at += (long)it * c.Hkv;
       ++e;
       continue;
     }
-    const int b = e / nrt, rt = e % nrt, hk = (int)((x - at) / it), i0 = (int)((x - at) % it);
+    const int hk = (int)(x - at) / it, i0 = (int)(x - at) % it;  // below 2^31: steps * 256 heads
     const int ni = (int)min((long)(it - i0), x1 - x);
     x += ni;
-    const Span sp = span_of(a, b);
     const int end = keys_end(a, sp, rt, TR);
     const int vis_all = sp.bad ? 0 : sp.P + (a.mask ? 0 : rt * TR / G + 1);  // keys every row sees
     const int32_t *table = c.pages + (size_t)b * c.max_pages;
     const int kbeg = i0 * IK + grp * TK;
     // the group's tiles: keys kbeg + j * IK, j < nj (as many rounds for every group)
     const int nj = i0 < steps && end > 0 ? min(ni, steps - i0) : 0;
-    auto has = [&](int j) __attribute__((always_inline)) { return j < nj && kbeg + j * IK < end; };
-    if (has(0)) {
-      tile.pages(c, table, kbeg, end);
-      tile.load(c, table, hk, 0, kbeg, end);
-    }
+    const int own = kbeg < end ? min(nj, (end - kbeg + IK - 1) / IK) : 0;
+    auto has = [&](int j) __attribute__((always_inline)) { return j < own; };
     // this lane's row: node, head, and q, a 16-byte piece per step: the right operand
     const int row = rt * TR + MF * rw + n, rowc = min(row, sp.live - 1);
     const int node = rowc / G, head = hk * G + rowc % G;
@@ -466,33 +473,24 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
 #pragma unroll
       for (int cc = 0; cc < NC; ++cc) qf[cc] = *reinterpret_cast<const u32x4 *>((const char *)qp + 16 * (NG * cc + h));
     }
+    if (has(0)) {
+      tile.pages(c, table, kbeg, end);
+      tile.load(c, table, hk, 0, kbeg, end);
+    }
     const bool wlive = rt * TR + MF * rw < sp.live;  // some row of this wave is there
     const float scl = a.scale * kLog2e;
     float m = -INFINITY, l = 0.f;  // running maximum (log2 units) and sum
     V o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = V(0.f);
-    uint32_t pw[NPW];      // probabilities as the second product takes them
+    uint32_t pw[NPW];           // probabilities as the second product takes them
     u32x2 vf[NR / 8 * NDT][2];  // bf16: values of 32 keys
-    uint32_t seen = ~0u;   // bit r: register r's key is seen
-
-    // Tile j + 1 into its buffer, between barriers j and j + 1: tile j - 1's readers
-    // are past barrier j.  (A wave that shares its tiles with no other needs one
-    // buffer: its reads of tile j come before.)
-    uint32_t odd_own = 0;  // bit: this wave's part of the tile in that buffer holds a value that is not finite
-    auto put = [&](int j) __attribute__((always_inline)) {
-      const int k0 = kbeg + j * IK, at_buf = j % Sh::NBUF;
-      unsigned char *kb = bufs + at_buf * Sh::BUF;
-      if (k0 + TK > vis_all || tile.badp != 0) {
-        const bool odd = __builtin_amdgcn_ballot_w64(tile.template store<true>(kb, end - k0)) != 0;
-        if (RW > 1 && lane == 0) s_odd[at_buf][wave] = odd;
-        odd_own = (odd_own & ~(1u << at_buf)) | (uint32_t)odd << at_buf;
-      } else {
-        tile.template store<false>(kb, 0);
-      }
-    };
+    // A masked tile that holds an infinity or NaN among its values, and those after
+    // it, are left for the end: 0 * inf would come through the product to rows that
+    // do not see the key.
+    int j_odd = own;
     // S^T = K Q^T, then probabilities and their sum.
-    auto scores = [&](int j, int u, auto kMasked) __attribute__((always_inline)) {
+    auto scores = [&](int j, int u) __attribute__((always_inline)) {
       const int k0 = kbeg + j * IK + 32 * u;
       // piece NG cc + h of row n: ^ 16 NG cc
       const uint32_t ka = opaque(bufs_at + (j % Sh::NBUF) * Sh::BUF + 32 * u * Sh::RB + 16 * piece_at<VPR>(n, h));
@@ -540,7 +538,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       float s[NR];
 #pragma unroll
       for (int r = 0; r < NR; ++r) s[r] = sv[r / (4 * NQ)][r % (4 * NQ)] * scl - mr;
-      if constexpr (decltype(kMasked)::value) {
+      if (k0 + 32 > vis_all) {
         const uint8_t *mp = opaque(a.mask ? a.mask + ((size_t)b * a.T + node) * a.T : nullptr);
         const int c0 = opaque(k0 - sp.P + 4 * h);
         uint32_t sn = 0;
@@ -555,7 +553,6 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
             sn |= ((uint32_t)(cn + v < 0) | (inside & in_mask)) << (4 * i + v);
           }
         }
-        seen = sn;
 #pragma unroll
         for (int r = 0; r < NR; ++r) s[r] = (sn >> r & 1) ? s[r] : -INFINITY;
       }
@@ -592,54 +589,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       }
     };
     // O^T += V^T P^T.
-    auto values = [&](int j, int u, auto kMasked) __attribute__((always_inline)) {
-      const uint32_t vb = bufs_at + (j % Sh::NBUF) * Sh::BUF + (TK + 32 * u) * Sh::RB;
-      bool odd = false;
-      if constexpr (decltype(kMasked)::value) {
-        odd = odd_own >> (j % Sh::NBUF) & 1;
-        if constexpr (RW > 1) {
-#pragma unroll
-          for (int w = 0; w < RW; ++w) odd |= s_odd[j % Sh::NBUF][grp * RW + w] != 0;
-        }
-      }
-      if (odd) {
-        // a value row that some row does not see may hold an infinity or NaN: key by
-        // key, every row over the keys it sees
-#pragma unroll 1
-        for (int key = 0; key < 32; ++key) {
-          const int hh = opaque(h), r0 = key / (4 * NG) * 4 + (key & 3), from = n + MF * (key / 4 % NG);
-          uint32_t w = 0;
-#pragma unroll
-          for (int r = 0; r < NPW; ++r)
-            if (r == (sizeof(T) == 2 ? r0 / 2 : r0)) w = pw[r];
-          w = __shfl(w, from, 64);
-          const uint32_t sn = __shfl(seen, from, 64);
-          const float p =
-              sizeof(T) == 4 ? __uint_as_float(w) : __uint_as_float((r0 & 1) ? w & 0xffff0000u : w << 16);
-          const bool vis = sn >> r0 & 1;
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) {
-#pragma unroll
-            for (int g8 = 0; g8 < NQ; ++g8) {
-              const int by = (MF * dt + 4 * (NG * g8 + hh)) * (int)sizeof(T);
-              const uint32_t va = vb + 16 * piece_at<VPR>(key, by / 16) + by % 16;
-              f32x4 vw;
-              if constexpr (sizeof(T) == 2) {
-                const u32x2 w2 = lds_read<u32x2>(va);
-                vw = f32x4{__uint_as_float(w2.x << 16), __uint_as_float(w2.x & 0xffff0000u),
-                           __uint_as_float(w2.y << 16), __uint_as_float(w2.y & 0xffff0000u)};
-              } else {
-                vw = lds_read<f32x4>(va);
-              }
-#pragma unroll
-              for (int w4 = 0; w4 < 4; ++w4)
-                o[dt][4 * g8 + w4] = vis ? o[dt][4 * g8 + w4] + p * vw[w4] : o[dt][4 * g8 + w4];
-            }
-            __builtin_amdgcn_sched_barrier(0);  // no loads ahead: registers are short here
-          }
-        }
-        return;
-      }
+    auto values = [&](int j, int u) __attribute__((always_inline)) {
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < NR / 4; i += 2) {
@@ -651,6 +601,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
           }
         }
       } else {
+        const uint32_t vb = bufs_at + (j % Sh::NBUF) * Sh::BUF + (TK + 32 * u) * Sh::RB;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
           const int key = 4 * (NG * (r / 4) + h) + r % 4;
@@ -663,32 +614,95 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
         }
       }
     };
-    if (has(0)) put(0);
-    if (has(1)) tile.load(c, table, hk, 1, kbeg + IK, end);
-    auto step = [&](int j, auto kMasked) __attribute__((always_inline)) {
-      if constexpr (RW > 1) __syncthreads();
-      if (decltype(kMasked)::value && !has(j)) return;
-      if (wlive) {
-        scores(j, 0, kMasked);
-        values(j, 0, kMasked);
-      }
-      if (has(j + 1)) put(j + 1);
-      if (has(j + 2)) tile.load(c, table, hk, j + 2, kbeg + (j + 2) * IK, end);
-      if (wlive) {
+    // One copy of everything in one loop: a workgroup runs through its code once or a
+    // few times, and fetching it is a part of what a short call takes.
 #pragma unroll 1
-        for (int u = 1; u < NS; ++u) {
-          scores(j, u, kMasked);
-          values(j, u, kMasked);
+    for (int j = 0; j < nj; ++j) {
+      const int at_buf = j % Sh::NBUF;
+      const bool masked = kbeg + j * IK + TK > vis_all;
+      bool odd = false;
+      if (has(j)) {
+        // Into the buffer of tile j - NBUF: with two, its readers are past barrier j - 1
+        // (a wave that shares its tiles with no other needs one).
+        const uint32_t to = bufs_at + at_buf * Sh::BUF;
+        if (masked || tile.badp != 0)
+          odd = __builtin_amdgcn_ballot_w64(tile.template store<true>(to, end - kbeg - j * IK)) != 0;
+        else
+          tile.template store<false>(to, 0);
+        // past the end the last tile again: a condition here would have the compiler
+        // move registers that are still being loaded, and wait for them
+        const int jl = min(j + 1, own - 1);
+        tile.load(c, table, hk, jl, kbeg + jl * IK, end);
+      }
+      if constexpr (RW > 1) {
+        if (masked && lane == 0) s_odd[at_buf][wave] = odd;
+        __syncthreads();
+        if (masked) {
+#pragma unroll
+          for (int w = 0; w < RW; ++w) odd |= s_odd[at_buf][grp * RW + w] != 0;
         }
       }
-    };
-    // whole tiles that every row sees, then the others
-    const int room = vis_all - TK - kbeg;
-    const int jm = room < 0 ? 0 : min(nj, room / IK + 1);
+      if (odd && masked) j_odd = min(j_odd, j);
+      if (!wlive || j >= j_odd) continue;
 #pragma unroll 1
-    for (int j = 0; j < jm; ++j) step(j, std::false_type{});
+      for (int u = 0; u < NS; ++u) {
+        scores(j, u);
+        values(j, u);
+      }
+    }
+    // The tiles that were left: a key at a time, from memory, every row over the keys
+    // it sees.
+    if (j_odd < own && wlive) {
 #pragma unroll 1
-    for (int j = jm; j < nj; ++j) step(j, std::true_type{});
+      for (int i = 0; i < (own - j_odd) * TK; ++i) {
+        const int pos = kbeg + (j_odd + i / TK) * IK + i % TK, cn = pos - sp.P;
+        if (pos >= end) continue;
+        const int first = uniform(Loads::runs1(c, table, pos));
+        const long r = max(first, 0);
+        const S *kr = (const S *)c.k + (r * c.Hkv + hk) * D, *vr = (const S *)c.v + (r * c.Hkv + hk) * D;
+        const float ks = sizeof(S) == 1 ? scale_of(c.ks[hk * c.rows() + r]) : 1.f;
+        const float vs = sizeof(S) == 1 ? scale_of(c.vs[hk * c.rows() + r]) : 1.f;
+        float dot = 0.f;
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc) {
+          constexpr int EP = 16 / sizeof(T);  // q's values in a piece
+#pragma unroll
+          for (int w = 0; w < EP; w += 4) {
+            const f32x4 kv = load4<S>(kr + EP * (NG * cc + h) + w);
+            f32x4 qv;
+            if constexpr (sizeof(T) == 4) {
+              qv = __builtin_bit_cast(f32x4, qf[cc]);
+            } else {
+              const uint32_t q0 = qf[cc][w / 2], q1 = qf[cc][w / 2 + 1];
+              qv = f32x4{__uint_as_float(q0 << 16), __uint_as_float(q0 & 0xffff0000u), __uint_as_float(q1 << 16),
+                         __uint_as_float(q1 & 0xffff0000u)};
+            }
+            dot += qv.x * kv.x + qv.y * kv.y + qv.z * kv.z + qv.w * kv.w;
+          }
+        }
+        if constexpr (MF == 16) dot = xor16_sum(dot);
+        dot = xor32_sum(dot) * ks * scl;
+        if (first < 0) dot = __int_as_float(0x7fc00000);
+        const bool vis =
+            cn < 0 || (a.mask ? a.mask[((size_t)b * a.T + node) * a.T + cn] != 0 : cn <= node);
+        const float mn = vis ? fmaxf(m, dot) : m, mr = mn == -INFINITY ? 0.f : mn;
+        const float alpha = sexp2(m, mr), p = vis ? __builtin_amdgcn_exp2f(dot - mr) : 0.f;
+        m = mn;
+        l = l * alpha + (h == 0 ? p : 0.f);  // the groups' sums are added up below
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int q4 = 0; q4 < NQ; ++q4) {
+            const f32x4 vv = load4<S>(vr + MF * dt + 4 * (NG * q4 + h));
+#pragma unroll
+            for (int w4 = 0; w4 < 4; ++w4) {
+              const float old = o[dt][4 * q4 + w4] * alpha;
+              o[dt][4 * q4 + w4] = vis ? old + p * (vv[w4] * vs) : old;
+            }
+            __builtin_amdgcn_sched_barrier(0);  // few registers: this is seldom run
+          }
+      }
+    }
     if constexpr (MF == 16) l = xor16_sum(l);
     l = xor32_sum(l);
 
