@@ -29,6 +29,7 @@
 //    holds one is added key by key, each row over the keys it sees.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "fe_attn_unit.h"
 #include "fe_paged.h"
@@ -150,14 +151,16 @@ struct Ranges {
 };
 
 // Workspace: per range two partials (slot 2w: the segment the range starts inside
-// of, 2w + 1: the one it ends inside of), o [TR][D] and (max, sum) [TR] each; then
-// the items before every (sequence, row tile), E + 1 of them.
+// of, 2w + 1: the one it ends inside of): the accumulators of RW waves as the lanes
+// hold them, [wave][D / MF][registers / 4][lane][4], so that writing and reading them
+// is one run of memory, and a row's (max, sum), [TR]; then the items before every
+// (sequence, row tile), E + 1 of them.
 template <int D> struct Work {
   float *p;
   long slots;
   int TR;
-  __host__ __device__ float *o(long slot) const { return p + slot * TR * D; }
-  __host__ __device__ float *ml(long slot) const { return p + slots * TR * D + slot * TR * 2; }
+  __device__ f32x4 *o(long slot) const { return (f32x4 *)(p + slot * TR * D); }
+  __device__ float2 *ml(long slot) const { return (float2 *)(p + slots * TR * D) + slot * TR; }
   __host__ __device__ long *before() const { return (long *)(p + slots * TR * (D + 2)); }
 };
 
@@ -764,77 +767,94 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
           }
       } else {
         const long slot = 2L * wg + (i0 > 0 ? 0 : 1);
-        const int rr = MF * rw + n;
-        float *po = work.o(slot) + (long)rr * D + 4 * h;
+        f32x4 *po = work.o(slot) + rw * NDT * NQ * 64 + lane;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
           for (int g8 = 0; g8 < NQ; ++g8)
-            *reinterpret_cast<f32x4 *>(po + MF * dt + 4 * NG * g8) =
-                f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
-        if (h == 0) *reinterpret_cast<float2 *>(work.ml(slot) + 2 * rr) = float2{m, l};
+            po[(NQ * dt + g8) * 64] = f32x4{o[dt][4 * g8], o[dt][4 * g8 + 1], o[dt][4 * g8 + 2], o[dt][4 * g8 + 3]};
+        if (h == 0) work.ml(slot)[MF * rw + n] = float2{m, l};
       }
     }
     __syncthreads();  // LDS is free for the next segment
   }
 }
 
-// Joins the partials of one segment in the order of their ranges: a workgroup per
-// (sequence, row tile, KV head) and 1024 / D rows, four dims a thread.
-template <typename T, int D>
+// Joins the partials of one segment in the order of their ranges: a wave per MF rows
+// and MF dims, a lane as it was in the kernel above, and as many waves of segment
+// (sequence, row tile, KV head) blockIdx.x as hold it.  Bound by the partials' bytes.
+template <typename T, int D, int MF>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int nrt, int W_, int TR) {
-  constexpr int RPW = 1024 / D;
+  constexpr int NDT = D / MF, NG = 64 / MF, NQ = MF * MF / 256, AT = 8 / NQ;
   const PagedView &c = a.c;
   const Work<D> work{a.ws, 2L * W_, TR};
   const int E = a.B * nrt, e = blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv;
-  const long before = work.before()[e], it = work.before()[e + 1] - before;
+  const long all = work.before()[E], before = work.before()[e], it = work.before()[e + 1] - before;
+  const Span sp = span_of(a, e / nrt);
   if (it == 0) return;
-  const Ranges rg(work.before()[E] * c.Hkv, W_);
+  const Ranges rg(all * c.Hkv, W_);
   const long S = before * c.Hkv + hk * it;
   const long w0 = rg.owner(S), w1 = rg.owner(S + it - 1);
   if (w0 == w1) return;  // one range held it all and wrote the rows
-  const Span sp = span_of(a, e / nrt);
-  const int rr = blockIdx.y * RPW + threadIdx.x / (D / 4), d0 = 4 * (threadIdx.x % (D / 4));
-  const int row = (e % nrt) * TR + rr;
-  if (rr >= TR || row >= sp.live) return;
-  auto slot = [&](long w) { return w == w0 ? 2 * w + 1 : 2 * w; };
-  // the row's D / 4 lanes hold a partial's maximum and sum each, then take turns
-  // handing out the weights
-  constexpr int GL = D / 4;
-  const int gl = threadIdx.x % GL;
-  float M = -INFINITY;
-  for (long w = w0; w <= w1; w += GL)
-    if (w + gl <= w1) M = fmaxf(M, work.ml(slot(w + gl))[2 * rr]);
-  M = group_max<GL>(M);
-  float L = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (long w = w0; w <= w1; w += GL) {
-    const int n = (int)min((long)GL, w1 + 1 - w);
-    float2 ml = {-INFINITY, 0.f};
-    if (gl < n) ml = *reinterpret_cast<const float2 *>(work.ml(slot(w + gl)) + 2 * rr);
-    const float sc = sexp2(ml.x, M);
-    L += ml.y * sc;
-    for (int i = 0; i < n; i += 8) {
-      f32x4 part[8];
+  const int lane = threadIdx.x & 63, n = lane % MF, h = lane / MF;
+  const int unit = uniform((int)(blockIdx.y * 4 + (threadIdx.x >> 6))), rw = unit / NDT, dt = unit % NDT;
+  const int row = (e % nrt) * TR + MF * rw + n;
+  if (row >= sp.live || MF * rw >= TR) return;
+  // o += the parts' sums, l += theirs, over the running maximum m; AT parts at a time
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[NQ];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        part[u] = *reinterpret_cast<const f32x4 *>(work.o(slot(w + min(i + u, n - 1))) + (long)rr * D + d0);
+  for (int q = 0; q < NQ; ++q) o[q] = f32x4(0.f);
+  auto add = [&](long w, auto kParts) __attribute__((always_inline)) {
+    constexpr int N = decltype(kParts)::value;
+    float2 ml[N];
+    f32x4 part[N][NQ];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float su = __shfl(sc, min(i + u, GL - 1), GL);
-        if (i + u < n && su > 0.f) o += part[u] * su;
-      }
+    for (int u = 0; u < N; ++u) {
+      const long slot = w + u == w0 ? 2 * w0 + 1 : 2 * (w + u);
+      ml[u] = work.ml(slot)[MF * rw + n];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) part[u][q] = work.o(slot)[(NQ * unit + q) * 64 + lane];
     }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < N; ++u) mn = fmaxf(mn, ml[u].x);
+    const float sc = sexp2(m, mn);
+    m = mn;
+    l *= sc;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) o[q] *= sc;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const float su = sexp2(ml[u].x, m);
+      l += ml[u].y * su;
+      // a part of no weight may hold anything
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) o[q] += su > 0.f ? part[u][q] * su : f32x4(0.f);
+    }
+  };
+  long w = w0;
+  for (; w + AT <= w1 + 1; w += AT) add(w, std::integral_constant<int, AT>());
+  if (AT > 4 && w + 4 <= w1 + 1) {
+    add(w, std::integral_constant<int, 4>());
+    w += 4;
   }
-  L = group_sum<GL>(L);
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  o *= inv;
+  if (AT > 2 && w + 2 <= w1 + 1) {
+    add(w, std::integral_constant<int, 2>());
+    w += 2;
+  }
+  if (w <= w1) add(w, std::integral_constant<int, 1>());
+  const float inv = sp.bad ? __int_as_float(0x7fc00000) : l == 0.f ? 0.f : 1.f / l;
   const int G = a.Hq / c.Hkv;
-  T *op = (T *)a.out + (((long)(e / nrt) * a.T + row / G) * a.Hq + hk * G + row % G) * D + d0;
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<u32x2 *>(op) = u32x2{f2bf2(o.x, o.y), f2bf2(o.z, o.w)};
-  else
-    *reinterpret_cast<f32x4 *>(op) = o;
+  T *op = (T *)a.out + (((long)(e / nrt) * a.T + row / G) * a.Hq + hk * G + row % G) * D + MF * dt + 4 * h;
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    const f32x4 y = o[q] * inv;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<u32x2 *>(op + 4 * NG * q) = u32x2{f2bf2(y.x, y.y), f2bf2(y.z, y.w)};
+    else
+      *reinterpret_cast<f32x4 *>(op + 4 * NG * q) = y;
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------
@@ -888,8 +908,8 @@ template <typename T, typename S, int D, int V> hipError_t launch(const TreeArgs
   k_tree_attn<T, S, D, Sh::MF, Sh::RW, Sh::KW><<<p.W, Sh::NT, 0, s>>>(a, p.nrt, p.W);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.join) return e;
-  const int rows = std::min<long>(Sh::TR, (long)a.T * (a.Hq / a.c.Hkv));
-  k_tree_join<T, D><<<dim3(a.B * p.nrt * a.c.Hkv, (rows * D + 1023) / 1024), 256, 0, s>>>(a, p.nrt, p.W, Sh::TR);
+  const int waves = std::min<long>(Sh::RW, ((long)a.T * (a.Hq / a.c.Hkv) + Sh::MF - 1) / Sh::MF) * (D / Sh::MF);
+  k_tree_join<T, D, Sh::MF><<<dim3(a.B * p.nrt * a.c.Hkv, (waves + 3) / 4), 256, 0, s>>>(a, p.nrt, p.W, Sh::TR);
   return hipGetLastError();
 }
 
