@@ -2,10 +2,14 @@
 // appended (rotated, kept as they are or coded in 8 bits), read back, and moved
 // behind the prefix after acceptance (gfx950).  All three are bound by bytes (or,
 // for a few rows, by the latency of one launch).
+#include <algorithm>
+
 #include "fe_paged.h"
 
 namespace fe {
 namespace {
+
+constexpr int kFewRows = 256;
 
 // ---- append -----------------------------------------------------------------------
 // One workgroup per new row (b, i): the row's angles once (double precision, 8
@@ -41,7 +45,7 @@ __global__ __launch_bounds__(256) void k_cache_append(PagedView c, int T_, const
   }
   const int d0 = 8 * (threadIdx.x % LPH), half = rope.rot / 2;
   const int nq = q ? Hq : 0, units = nq + 2 * c.Hkv;
-  for (int u = threadIdx.x / LPH; u < units; u += 256 / LPH) {
+  for (int u = blockIdx.y * (256 / LPH) + threadIdx.x / LPH; u < units; u += gridDim.y * (256 / LPH)) {
     const int kind = u < nq ? 0 : u < nq + c.Hkv ? 1 : 2;  // query, key, value
     const int h = kind == 0 ? u : kind == 1 ? u - nq : u - nq - c.Hkv;
     const T *src = (kind == 0 ? q + r * qs : kind == 1 ? k + r * ks : v + r * vs) + (long)h * D;
@@ -121,33 +125,41 @@ __device__ __forceinline__ int seq_of(const int32_t *__restrict__ cu, int B, int
   return n;
 }
 
-// One workgroup per packed row and 256 of its 8-value pieces.
+// One wave per packed row, so that its sequence and page are wave-uniform; a lane
+// takes the same 16 bytes of stored keys and values (8 values of fp32) at a time.
 template <typename T, typename S, int D>
 __global__ __launch_bounds__(256) void k_cache_gather(PagedView c, int B, const int32_t *__restrict__ starts,
                                                       const int32_t *__restrict__ cu, int n_rows,
                                                       T *__restrict__ ko, T *__restrict__ vo) {
-  const int per = c.Hkv * (D / 8);  // pieces per row
-  for (int r = blockIdx.x; r < n_rows; r += gridDim.x) {
+  constexpr int NV = sizeof(S) == 1 ? 2 : 1;        // runs of 8 values
+  const int per = c.Hkv * (D / (8 * NV)), lane = threadIdx.x & 63;
+  for (int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); r < n_rows; r += gridDim.x * 4) {
     const int b = seq_of(cu, B, r);
     if (b >= B || r < cu[0]) continue;
     const long pos = (starts ? (long)starts[b] : 0) + r - cu[b];
     const long row = pos >= 0 && pos < c.max_len ? c.row(b, (int)pos) : -1;
-    for (int p = threadIdx.x; p < per; p += 256) {
-      const int h = p / (D / 8);
-      const long at = row * c.Hkv * D + 8 * p;
+    const long from = max(row, 0L) * c.Hkv * D, to = (long)r * c.Hkv * D;
+    for (int p = lane; p < per; p += 64) {
+      const int h = p / (D / (8 * NV));
+      f32x8 y[2][NV];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        T *dst = w ? vo : ko;
-        if (!dst) continue;
-        f32x8 y;
-        if (row < 0) {
-          y = f32x8(__int_as_float(0x7fc00000));
-        } else {
-          y = load8<S>((const S *)(w ? c.v : c.k) + at);
-          if constexpr (sizeof(S) == 1) y *= scale_of((w ? c.vs : c.ks)[h * c.rows() + row]);
+      for (int w = 0; w < 2; ++w)
+        if (w ? vo : ko) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) y[w][i] = load8<S>((const S *)(w ? c.v : c.k) + from + 8 * (NV * p + i));
+          if constexpr (sizeof(S) == 1) {
+            const float sc = scale_of((w ? c.vs : c.ks)[h * c.rows() + max(row, 0L)]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) y[w][i] *= sc;
+          }
         }
-        store8<T>(dst + (long)r * c.Hkv * D + 8 * p, y);
-      }
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+        if (T *dst = w ? vo : ko) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+            store8<T>(dst + to + 8 * (NV * p + i), row < 0 ? f32x8(__int_as_float(0x7fc00000)) : y[w][i]);
+        }
     }
   }
 }
@@ -221,8 +233,10 @@ template <typename T, bool F8, int D>
 hipError_t append_d(const PagedView &c, int B, int T_, const int32_t *starts, const int32_t *counts,
                     const int32_t *positions, const RopeArgs &rope, const void *k, long ks, const void *v,
                     long vs, const void *q, long qs, int Hq, void *q_out, hipStream_t s) {
+  // Few rows: their heads over as many workgroups as take them in one step.
+  const int heads = (q ? Hq : 0) + 2 * c.Hkv, split = B * T_ <= kFewRows ? (heads * (D / 8) + 255) / 256 : 1;
   auto go = [&](auto kern) {
-    kern<<<B * T_, 256, 0, s>>>(c, T_, starts, counts, positions, rope, (const T *)k, ks, (const T *)v, vs,
+    kern<<<dim3(B * T_, split), 256, 0, s>>>(c, T_, starts, counts, positions, rope, (const T *)k, ks, (const T *)v, vs,
                                 (const T *)q, qs, Hq, (T *)q_out);
     return hipGetLastError();
   };
@@ -232,7 +246,7 @@ hipError_t append_d(const PagedView &c, int B, int T_, const int32_t *starts, co
 template <typename T, typename S>
 hipError_t gather_t(const PagedView &c, int B, const int32_t *starts, const int32_t *cu, int n_rows, void *ko,
                     void *vo, hipStream_t s) {
-  const int grid = n_rows < 65536 ? n_rows : 65536;
+  const int grid = (int)std::min<long>(((long)n_rows + 3) / 4, 65536);
   if (c.D == 64)
     k_cache_gather<T, S, 64><<<grid, 256, 0, s>>>(c, B, starts, cu, n_rows, (T *)ko, (T *)vo);
   else
