@@ -880,19 +880,36 @@ struct Plan {
 };
 constexpr int kMaxCus = 512;
 
-// Variants by rows per (sequence, KV head): MF, RW, KW, workgroups per compute unit.
-// The last is fp32's, whose operands take twice the registers.
-constexpr int kShapes[6][4] = {{16, 1, 4, 2}, {32, 1, 4, 2}, {32, 2, 2, 2}, {32, 4, 2, 1}, {32, 8, 1, 1}, {32, 4, 1, 1}};
+// The variants: MF, RW, KW, workgroups per compute unit.  The last is fp32's, whose
+// operands take twice the registers.
+constexpr int kShapes[4][4] = {{16, 1, 4, 2}, {32, 4, 2, 1}, {32, 8, 1, 1}, {32, 4, 1, 1}};
 
-int variant_of(int rows, int dt) {
-  if (rows <= 16) return 0;
-  return dt == kF32 ? 5 : rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 3 : 4;
+// The variant for `rows` per (sequence, KV head) and `keys` over all of these.  Few
+// rows in all, counted in tiles of 16: a workgroup of 16 rows starts soonest and
+// leaves the smallest partial sums; more row tiles then read a key more often, from
+// L2.  Many: a key is staged once for 128 rows, or for 256, whose partial sums are
+// twice as large: up to 2^16 keys only where one tile holds all rows (204 rows over
+// 1024 keys: 26 us in tiles of 128, 22 in one of 256).  Measured with 8 KV heads of 128 dims and 2048 keys a
+// sequence (us; 16 / 128 / 256 rows at a time; * taken):
+//   rows   bf16, 1 seq.      bf16, 32            8 bits, 1         8 bits, 32
+//    16   *14 /  19 /  19    59 / *47 /   57    *12 / 19 /  18   *33 /  47 /   54
+//    32   *16 /  20 /  19    63 / *48 /   58    *14 / 20 /  19    39 / *47 /   55
+//   128    28 / *23 /  22   162 / *61 /   68    *17 / 23 /  22   133 / *54 /   62
+//   256    30 /  30 / *33   289 / 108 /  *93    *21 / 30 /  32   261 /  98 /  *83
+//   512    33 / *24 /  34   578 / 209 / *177     28 / *28 / 34   522 / 191 / *163
+// fp32, 32 sequences, 16 / 128 rows at a time: 16 rows 131 / 400, 32 rows 225 / 400,
+// 64 rows 424 / 405.
+int variant_of(int rows, int dt, bool f8, long keys) {
+  if (dt == kF32) return rows <= 32 ? 0 : 3;
+  const long tiles = (rows + 15) / 16;
+  if (f8 ? rows <= 16 || keys * tiles <= 1L << 18 : rows <= 32 && keys * tiles <= 1L << 17) return 0;
+  return rows <= 128 || (rows > 256 && keys <= 1L << 16) ? 1 : 2;
 }
 
 Plan plan_of(const PagedView &c, int B, int T, int Hq, int dt, int cus) {
   const int rows = T * (Hq / c.Hkv);
   Plan p;
-  p.variant = variant_of(rows, dt);
+  p.variant = variant_of(rows, dt, c.dtype == kF8, (long)B * c.Hkv * c.max_len);
   const int *sh = kShapes[p.variant];
   const int TR = sh[0] * sh[1], IK = sh[2] * tile_keys(sh[1], c.D);
   p.nrt = (rows + TR - 1) / TR;
@@ -916,12 +933,9 @@ template <typename T, typename S, int D, int V> hipError_t launch(const TreeArgs
 template <typename T, typename S, int D> hipError_t by_rows(const TreeArgs &a, const Plan &p, hipStream_t s) {
   if (p.variant == 0) return launch<T, S, D, 0>(a, p, s);
   if constexpr (sizeof(T) == 4)
-    return launch<T, S, D, 5>(a, p, s);
+    return launch<T, S, D, 3>(a, p, s);
   else
-    return p.variant == 1   ? launch<T, S, D, 1>(a, p, s)
-           : p.variant == 2 ? launch<T, S, D, 2>(a, p, s)
-           : p.variant == 3 ? launch<T, S, D, 3>(a, p, s)
-                            : launch<T, S, D, 4>(a, p, s);
+    return p.variant == 1 ? launch<T, S, D, 1>(a, p, s) : launch<T, S, D, 2>(a, p, s);
 }
 
 template <typename T, typename S> hipError_t by_dim(const TreeArgs &a, const Plan &p, hipStream_t s) {
