@@ -405,7 +405,8 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
   }
   total = uniform(total);
   segs = uniform(segs);
-  const int extra = total * c.Hkv > 2L * W_ ? kSegItems : 0;
+  // (with one item a segment is never cut, and no second launch joins it)
+  const int extra = c.max_len > IK && total * c.Hkv > 2L * W_ ? kSegItems : 0;
   const Ranges rg((total + (long)extra * segs) * c.Hkv, W_);
   if (rg.total == 0) {
     if (blockIdx.x == 0)
