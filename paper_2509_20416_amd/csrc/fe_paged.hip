@@ -9,14 +9,21 @@
 namespace fe {
 namespace {
 
-constexpr int kFewRows = 256;
-
 // ---- append -----------------------------------------------------------------------
 // One workgroup per new row (b, i): the row's angles once (double precision, 8
 // bytes of product and the sine and cosine of the reduced angle, so positions past
 // 2^24 turn by the right amount), shared by all its heads.  A lane takes 8
 // neighbouring dims of a head, so 16-byte loads and stores throughout; the other
-// half of its pairs (half layout) is a second load from the same lines.
+// half of its pairs (half layout) is a second load from the same lines.  Bound by
+// bytes: 8192 rows with 64 query and 8 KV heads of 128 dims, rotated, the cache in 8
+// bits, 319 MB in 63 us, 5.0 TB/s.
+//
+// Up to kFewRows rows their heads are spread over as many workgroups as take them in
+// one step, which computes the angles more often and waits for one load instead of
+// several (8 KV heads and 32 query heads of 128 dims, us, spread / not): 32 rows 4.0 /
+// 6.0, 256 rows 4.8 / 6.5, 512 rows 6.4 / 7.1, 1024 rows 9.4 / 8.5.
+constexpr int kFewRows = 512;
+
 template <typename T, bool F8, int D, bool ROPE>
 __global__ __launch_bounds__(256) void k_cache_append(PagedView c, int T_, const int32_t *__restrict__ starts,
                                                       const int32_t *__restrict__ counts,
@@ -127,6 +134,7 @@ __device__ __forceinline__ int seq_of(const int32_t *__restrict__ cu, int B, int
 
 // One wave per packed row, so that its sequence and page are wave-uniform; a lane
 // takes the same 16 bytes of stored keys and values (8 values of fp32) at a time.
+// Bound by bytes: 833 MB of 32 histories, 8 bits to bf16, in 176 us, 4.7 TB/s.
 template <typename T, typename S, int D>
 __global__ __launch_bounds__(256) void k_cache_gather(PagedView c, int B, const int32_t *__restrict__ starts,
                                                       const int32_t *__restrict__ cu, int n_rows,
@@ -171,7 +179,9 @@ struct CommitArgs {
 
 // One workgroup per (layer, sequence).  A thread owns 16-byte columns of the
 // rows: it loads its column of every source row before it stores any, so rows
-// that are both source and destination need no order between threads.
+// that are both source and destination need no order between threads.  Bound by
+// latency, lengths to table to rows: 4.8 us for one sequence in 5 layers, 9.2 us for
+// 32 in 32 layers (14.8 MB).
 __global__ __launch_bounds__(256) void k_cache_commit(PagedView c, CommitArgs a, int first, int T, int n_paths,
                                                       int depth, const int32_t *__restrict__ lens,
                                                       const int32_t *__restrict__ retrieve,
@@ -233,7 +243,6 @@ template <typename T, bool F8, int D>
 hipError_t append_d(const PagedView &c, int B, int T_, const int32_t *starts, const int32_t *counts,
                     const int32_t *positions, const RopeArgs &rope, const void *k, long ks, const void *v,
                     long vs, const void *q, long qs, int Hq, void *q_out, hipStream_t s) {
-  // Few rows: their heads over as many workgroups as take them in one step.
   const int heads = (q ? Hq : 0) + 2 * c.Hkv, split = B * T_ <= kFewRows ? (heads * (D / 8) + 255) / 256 : 1;
   auto go = [&](auto kern) {
     kern<<<dim3(B * T_, split), 256, 0, s>>>(c, T_, starts, counts, positions, rope, (const T *)k, ks, (const T *)v, vs,

@@ -3,30 +3,44 @@
 // The T * G rows of one (sequence, KV head) -- its nodes times the G query heads
 // that share the KV head -- read the same keys, so they are the columns of one
 // pair of matrix products over the cache: S^T = K Q^T, O^T = V^T P^T.  A
-// workgroup takes a tile of TR = 32 RW of these rows and walks the keys once,
-// with the running maximum and sum of a softmax per row.
+// workgroup takes a tile of TR of these rows and walks the keys once, with the
+// running maximum and sum of a softmax per row.
 //
-//  * In the 32x32 accumulators a lane holds 16 keys of one row, which is what the
-//    second product wants as its right operand once V's keys are taken in the
-//    same order: probabilities never move between lanes, and a row's maximum and
-//    sum need one exchange, with lane ^ 32.
-//  * Keys go through registers into LDS: a tile is loaded (16 bytes a lane, its
-//    pages looked up one tile ahead) while the one before is worked on, and 8-bit
-//    codes become bf16 (or fp32) there, once per workgroup.  With a power of two
-//    as the scale that is exact.
-//  * RW waves share a tile, side by side on rows; KW groups of them take the
-//    tiles in turn and add up at the end.  Few rows: RW = 1, every wave streams
-//    its own keys, which is a matter of bytes.  Many: RW = 4, each key is read
-//    once per 128 rows.
+//  * In the accumulators a lane holds keys of one row, which is what the second
+//    product wants as its right operand once V's keys are taken in the same order
+//    (the transposing LDS read delivers them so): probabilities never move between
+//    lanes, and a row's maximum and sum need an exchange with lane ^ 32 (and ^ 16
+//    in tiles of 16) only.
+//  * Keys go through registers into LDS: a tile is loaded (16 bytes a lane) while
+//    the one before is worked on, and 8-bit codes become bf16 (or fp32) there, once
+//    per workgroup.  With a power of two as the scale that is exact.
+//  * RW waves share a tile, side by side on rows; KW groups of them take the tiles
+//    in turn and add up at the end.  RW = 1: every wave streams keys of its own, one
+//    LDS buffer and no barrier.  RW = 4, 8: a key is staged once per 128 or 256 rows,
+//    in two buffers, one barrier a tile.
 //  * The tiles of all (sequence, row tile, KV head) segments are numbered and cut
 //    into equal ranges, one per workgroup, whatever the lengths: a segment that
 //    ranges share leaves partial sums, joined in order by a second launch.  A
 //    range leaves at most two partials (the segment it starts in and the one it
 //    ends in), so their number does not depend on the lengths either.
-//  * Only tiles that reach past what every row of the tile sees are masked.  A
-//    masked score is replaced, so what it was does not matter; in a value row an
-//    infinity or NaN would still come through as 0 * inf, so a masked tile that
-//    holds one is added key by key, each row over the keys it sees.
+//  * Only keys past what every row of the tile sees are masked.  A masked score is
+//    replaced, so what it was does not matter; in a value row an infinity or NaN
+//    would still come through as 0 * inf, so from a masked tile on that holds one,
+//    keys are added one by one at the end, each row over those it sees.
+//
+// Scores, probabilities' sum and accumulators are fp32; in bf16 the probabilities
+// are rounded as the matrix instruction takes them, and summed as rounded.
+//
+// What bounds it (the two launches under a kernel trace): few rows, the cache's
+// bytes -- 32 sequences, one token, 280 MB of 8-bit rows: 55 + 5 us, 4.7 TB/s, where
+// a copy reaches 5.2.  Many rows, the pipes that a tile goes through one after the
+// other: 1024 nodes of 32 heads behind 8192 keys, 146 GFLOP, 179 + 12 us, 765
+// TFLOP/s where a large library product reaches 1300; of 5900 cycles a tile (64
+// keys, 256 rows) the matrix pipe is busy for 2050, LDS reads and the softmax for
+// about as many each.  Reading the next keys' pieces under the softmax did not help
+// (173 -> 184 us: registers).  A few short sequences, latency: a workgroup's setup is
+// about 20000 cycles with its first keys' way from memory, and the partials' way
+// through memory costs 5 to 8 us more.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -114,7 +128,8 @@ __device__ __forceinline__ int keys_end(const TreeArgs &a, const Span &s, int rt
 // Starting and ending a segment costs about as much as kSegItems of its work items
 // (its lengths, pages, queries and first keys are fetched one after the other, and
 // its sums written), so where every workgroup gets several items a segment counts
-// that many more.
+// that many more.  With 0, 1, 2, 3, 5: one token each of 32 ragged histories 127, 111,
+// 100, 93, 95 us, 32 ragged trees 292, 269, 251, 240, 240 (as the kernels then were).
 constexpr int kSegItems = 3;
 
 // Work items of a segment: steps over its keys (none where the tile has no row).
@@ -783,7 +798,9 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
 
 // Joins the partials of one segment in the order of their ranges: a wave per MF rows
 // and MF dims, a lane as it was in the kernel above, and as many waves of segment
-// (sequence, row tile, KV head) blockIdx.x as hold it.  Bound by the partials' bytes.
+// (sequence, row tile, KV head) blockIdx.x as hold it.  Bound by the partials' bytes:
+// 17 us for up to 67 MB of them (256 ranges of 256 rows), 4 to 8 us where latency
+// counts.
 template <typename T, int D, int MF>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int nrt, int W_, int TR) {
   constexpr int NDT = D / MF, NG = 64 / MF, NQ = MF * MF / 256, AT = 8 / NQ;
