@@ -618,8 +618,8 @@ fe_status fe_cache_gather(const fe_paged_kv *cache, const fe_page_table *table, 
  * (fe_cache_append wrote them).  Node a sees the prefix and the nodes c < n with
  * mask[b][a][c] != 0 (mask NULL: c <= a, a causal run):
  *   out[b][a][h] = sum_j softmax_j(scale * q[b][a][h] . k_j) v_j,
- * head h reading KV head h / (n_q_heads / H_kv).  A node that sees nothing gets
- * zeros; what a node does not see never matters, infinities and NaN included.
+ * head h reading KV head h / (n_q_heads / H_kv).  A node that sees nothing, or
+ * only scores of minus infinity, gets zeros; what a node does not see never matters, infinities and NaN included.
  * The sums are fp32; in bf16 the probabilities are rounded to bf16 as they enter
  * the product with the values and in the sum that divides it.
  *  q    [B, nodes, n_q_heads, D] in dtype (FE_BF16 or FE_F32; the cache's dtype is
@@ -634,7 +634,8 @@ fe_status fe_cache_gather(const fe_paged_kv *cache, const fe_page_table *table, 
  * nodes] or P + n > max_len reads no cache row and its live rows (all, where n is
  * bad) become NaN; a key on a page outside [0, n_pages) is NaN to the nodes that
  * see it.  Rows from counts[b] on are left as they were.  n_q_heads is a multiple
- * of H_kv, at most 1024; nodes * n_q_heads / H_kv at most 2^20.  Errors:
+ * of H_kv, at most 1024; nodes * n_q_heads / H_kv at most 2^20, H_kv * max_len at
+ * most 2^36.  Errors:
  * FE_E_INVALID, FE_E_UNSUPPORTED, FE_E_ALIGN, FE_E_WORKSPACE; nothing is launched
  * on an error.  batch == 0 or nodes == 0 is a no-op. */
 fe_status fe_tree_attention(const fe_paged_kv *cache, const fe_page_table *table, int32_t batch,
@@ -654,7 +655,8 @@ size_t fe_tree_attention_workspace_bytes(const fe_paged_kv *cache, const fe_page
  * P + t takes what position P + path[t] held before the call, t = 1 .. len (keys
  * are rotated by depth, so they stay right), and new_lens[b] = P + 1 + len: the
  * root and the accepted nodes are verified.
- *  caches   HOST array [n_layers] (1 .. 1024), all of one shape, one page table
+ *  caches   HOST array [n_layers] (1 .. 1024), all of one shape, no two of the same
+ *           memory; one page table
  *  retrieve [B, n_paths, depth + 1] int32 (fe_tree_out.retrieve), depth 0 .. 16
  *  prefix_lens, accept_path, accept_len [B] int32; new_lens [B] int32, not
  *           overlapping them

@@ -141,8 +141,8 @@ __global__ __launch_bounds__(256) void k_cache_gather(PagedView c, int B, const 
                                                       T *__restrict__ ko, T *__restrict__ vo) {
   constexpr int NV = sizeof(S) == 1 ? 2 : 1;        // runs of 8 values
   const int per = c.Hkv * (D / (8 * NV)), lane = threadIdx.x & 63;
-  for (int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); r < n_rows; r += gridDim.x * 4) {
-    const int b = seq_of(cu, B, r);
+  for (long rl = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); rl < n_rows; rl += gridDim.x * 4) {
+    const int r = (int)rl, b = seq_of(cu, B, r);
     if (b >= B || r < cu[0]) continue;
     const long pos = (starts ? (long)starts[b] : 0) + r - cu[b];
     const long row = pos >= 0 && pos < c.max_len ? c.row(b, (int)pos) : -1;

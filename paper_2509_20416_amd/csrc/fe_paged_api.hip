@@ -108,6 +108,8 @@ fe_status check_attention(const fe_paged_kv *cache, const fe_page_table *table, 
   if (n_q_heads > 1024) return fail(FE_E_UNSUPPORTED, "n_q_heads > 1024");
   if ((int64_t)nodes * (n_q_heads / cache->n_kv_heads) > (1 << 20))
     return fail(FE_E_UNSUPPORTED, "nodes * n_q_heads / n_kv_heads > 2^20");
+  if ((int64_t)cache->n_kv_heads * table->max_len > (int64_t)1 << 36)
+    return fail(FE_E_UNSUPPORTED, "n_kv_heads * max_len > 2^36");
   return FE_OK;
 }
 
@@ -287,6 +289,10 @@ extern "C" fe_status fe_cache_commit(const fe_paged_kv *caches, int32_t n_layers
   for (const void *p : in)
     if (overlap(p, 4 * (int64_t)batch, new_lens, 4 * (int64_t)batch))
       return fail(FE_E_INVALID, "new_lens overlaps an input");
+  for (int l = 1; l < n_layers; ++l)
+    for (int m = 0; m < l; ++m)
+      if (pools[l].k == pools[m].k || pools[l].v == pools[m].v)
+        return fail(FE_E_INVALID, "layers %d and %d share a cache", m, l);
   FE_TRY(cache_commit(view(caches, table), pools, n_layers, batch, nodes, n_paths, depth, prefix_lens, retrieve,
                       accept_path, accept_len, new_lens, (hipStream_t)stream));
   return FE_OK;

@@ -472,7 +472,7 @@ __global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 2 ? 2 : 1) void k_tree_a
       ++e;
       continue;
     }
-    const int hk = (int)(x - at) / it, i0 = (int)(x - at) % it;  // below 2^31: steps * 256 heads
+    const int hk = (int)(x - at) / it, i0 = (int)(x - at) % it;  // below 2^31: keys * heads are at most 2^36
     const int ni = (int)min((long)(it - i0), x1 - x);
     x += ni;
     const int end = keys_end(a, sp, rt, TR);
